@@ -351,6 +351,37 @@ int sqnn_store_probe(void *d_out, size_t bytes, uint32_t chunk_bytes, void *cuda
  * after it, process-wide. */
 void sqnn_set_debug_flags(uint32_t flags, uint64_t wait_limit_cycles);
 
+/* ---- layers in 8-bit floating point ------------------------------------------------------------
+ *
+ * What a model needs beside its encrypted layers (the paper has no counterpart): layers whose weights
+ * are kept as e4m3 numbers (sign, four exponent bits of bias 7, three mantissa bits, largest 448, no
+ * infinity, 0x7f and 0xff are NaN) with one fp32 scale for each block of SQNN_FP8_BLOCK x
+ * SQNN_FP8_BLOCK weights, and activations as e4m3 numbers with one fp32 scale for each row and
+ * SQNN_FP8_BLOCK columns.  A number stands for itself times its scale; blocks at the right and lower
+ * edge may be partial.  All strides are in elements. */
+#define SQNN_FP8_BLOCK 128
+
+/* Root-mean-square norm with the residual's addition and an 8-bit output: for each of `batch` rows of n
+ *   h = x + residual, rounded once to the residual's type, written to d_h   (no residual: h = x)
+ *   y = h / sqrt(mean(h^2) + eps) * weight
+ *   scale[k] = max |y| of columns 128 k .. 128 k + 127, over 448, as fp32, 2^-126 at least
+ *   q = y / scale, rounded once to e4m3 (nearest, ties to even)
+ * d_residual and d_h: both or neither, of residual_dtype.  d_q with d_scale ([batch][ceil(n / 128)], row
+ * stride lds), or d_y (y_dtype), or all three are written.  Types SQNN_X_F32 or SQNN_X_BF16 (the fp32 output
+ * of the products is a valid x beside a bf16 residual).  h, scale and q are what the formulas give in exact
+ * arithmetic, whatever the sizes (but for values within 2^-50 or so of a border), so results do not depend on the order of a
+ * sum; y is within two last places of fp32, rounded to its type.  A NaN or an infinity
+ * in a row of h makes NaN of its columns' groups (scale and q) and of y there; what else is in
+ * such a row follows from the formulas.  d_h may be d_residual or d_x and d_y may be d_x where type and
+ * stride are the same; otherwise outputs must not overlap inputs.  Any alignment and stride is served; rows of x,
+ * residual, h and y on 16-byte boundaries, q on 8, are faster.  One kernel, nothing allocated.
+ * Errors: INVALID_ARG (NULL, sizes, strides below n, types, eps negative or NaN), UNSUPPORTED (n above 2^30), CUDA. */
+int sqnn_rmsnorm_fp8(uint32_t batch, uint64_t n, const void *d_x, int x_dtype, int64_t ldx,
+                     const void *d_residual, int residual_dtype, int64_t ldr, void *d_h, int64_t ldh,
+                     const void *d_weight, int weight_dtype, double eps,
+                     uint8_t *d_q, int64_t ldq, float *d_scale, int64_t lds,
+                     void *d_y, int y_dtype, int64_t ldy, void *cuda_stream);
+
 /* Scratch bytes sqnn_decode_matmul needs for this layer and batch (0 for batch <= 15). */
 size_t sqnn_workspace_bytes(const sqnn_desc *desc, uint32_t batch);
 

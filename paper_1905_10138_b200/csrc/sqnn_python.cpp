@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -19,18 +20,20 @@ namespace {
 decltype(&sqnn_decode) f_decode = nullptr;
 decltype(&sqnn_decode_matmul) f_matmul = nullptr;
 decltype(&sqnn_decode_matmul_static) f_matmul_static = nullptr;
+decltype(&sqnn_rmsnorm_fp8) f_rmsnorm_fp8 = nullptr;
 
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    if (nargs != 3) { PyErr_SetString(PyExc_TypeError, "bind takes three addresses"); return nullptr; }
-    void *p[3];
-    for (int i = 0; i < 3; ++i) {
+    if (nargs != 4) { PyErr_SetString(PyExc_TypeError, "bind takes four addresses"); return nullptr; }
+    void *p[4];
+    for (int i = 0; i < 4; ++i) {
         p[i] = PyLong_AsVoidPtr(args[i]);
         if (PyErr_Occurred()) return nullptr;
     }
     f_decode = reinterpret_cast<decltype(f_decode)>(p[0]);
     f_matmul = reinterpret_cast<decltype(f_matmul)>(p[1]);
     f_matmul_static = reinterpret_cast<decltype(f_matmul_static)>(p[2]);
+    f_rmsnorm_fp8 = reinterpret_cast<decltype(f_rmsnorm_fp8)>(p[3]);
     Py_RETURN_NONE;
 }
 
@@ -214,11 +217,99 @@ PyObject *matmul_static(PyObject *, PyObject *const *a, Py_ssize_t nargs)
     });
 }
 
+// ---- layers in 8-bit floating point.  Their tensors are checked here: where they are, their types and shapes.
+
+bool fail(const char *what)
+{
+    PyErr_SetString(PyExc_ValueError, what);
+    return false;
+}
+bool on_device(const at::Tensor *t, const char *name)
+{
+    if (!t) return true;
+    if (t->is_cuda() && t->get_device() == c10::cuda::current_device()) return true;
+    PyErr_Format(PyExc_ValueError, "%s must be on the current CUDA device", name);
+    return false;
+}
+// A matrix whose rows are contiguous; `rows` or `cols` < 0: any.
+bool matrix(const at::Tensor *t, int64_t rows, int64_t cols, const char *name)
+{
+    if (!on_device(t, name)) return false;
+    if (t->dim() == 2 && (rows < 0 || t->size(0) == rows) && (cols < 0 || t->size(1) == cols) && (t->size(1) == 1 || t->stride(1) == 1))
+        return true;
+    PyErr_Format(PyExc_ValueError, "%s must be a matrix of the right size with unit inner stride", name);
+    return false;
+}
+// Row stride; the one row of a matrix has whatever torch says, so it gets one that suits every check.
+int64_t row_stride(const at::Tensor *t) { return t->size(0) == 1 ? (t->size(1) + 15) / 16 * 16 : t->stride(0); }
+bool real_type(const at::Tensor *t, int *dtype, const char *name)
+{
+    if (t->scalar_type() == at::kFloat) *dtype = SQNN_X_F32;
+    else if (t->scalar_type() == at::kBFloat16) *dtype = SQNN_X_BF16;
+    else {
+        PyErr_Format(PyExc_ValueError, "%s must be float32 or bfloat16", name);
+        return false;
+    }
+    return true;
+}
+bool of_type(const at::Tensor *t, at::ScalarType type, const char *name)
+{
+    if (t->scalar_type() == type) return true;
+    PyErr_Format(PyExc_ValueError, "%s must be %s", name, at::toString(type));
+    return false;
+}
+constexpr int64_t blocks_of(int64_t n) { return (n + SQNN_FP8_BLOCK - 1) / SQNN_FP8_BLOCK; }
+
+// rmsnorm_fp8(x, weight, eps, q, scale, residual, h, y, stream) -> status code
+PyObject *rmsnorm_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return guarded([&]() -> PyObject * {
+        if (!enough(nargs, 9)) return nullptr;
+        const at::Tensor *x, *w, *q, *scale, *r, *h, *y;
+        void *st;
+        if (!tensor_arg(a[0], &x) || !tensor_arg(a[1], &w) || !tensor_arg(a[3], &q) || !tensor_arg(a[4], &scale) ||
+            !tensor_arg(a[5], &r) || !tensor_arg(a[6], &h) || !tensor_arg(a[7], &y))
+            return nullptr;
+        const double eps = PyFloat_AsDouble(a[2]);
+        if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+        if (!x || !w) { fail("x and weight are required"); return nullptr; }
+        if (!matrix(x, -1, -1, "x")) return nullptr;
+        const int64_t batch = x->size(0), n = x->size(1);
+        int xt, wt, rt = SQNN_X_F32, yt = SQNN_X_F32;
+        if (!real_type(x, &xt, "x") || !real_type(w, &wt, "weight") || !on_device(w, "weight")) return nullptr;
+        if (w->dim() != 1 || w->size(0) != n || (n > 1 && w->stride(0) != 1)) { fail("weight must be a vector as long as a row of x"); return nullptr; }
+        if (q && (!matrix(q, batch, n, "q") || !of_type(q, at::kFloat8_e4m3fn, "q"))) return nullptr;
+        if (scale && (!matrix(scale, batch, blocks_of(n), "scale") || !of_type(scale, at::kFloat, "scale"))) return nullptr;
+        if (r && (!matrix(r, batch, n, "residual") || !real_type(r, &rt, "residual"))) return nullptr;
+        if (h && (!matrix(h, batch, n, "h") || !r || !of_type(h, r->scalar_type(), "h"))) {
+            if (!PyErr_Occurred()) fail("h goes with a residual");
+            return nullptr;
+        }
+        if (y && (!matrix(y, batch, n, "y") || !real_type(y, &yt, "y"))) return nullptr;
+        if (batch > 0x7fffffff) { fail("too many rows"); return nullptr; }
+        if (!stream_arg(a[8], &st)) return nullptr;
+        const auto ld = [](const at::Tensor *t) { return t ? row_stride(t) : 0; };
+        const void *const p_x = ptr<void>(x), *const p_r = ptr<void>(r), *const p_w = ptr<void>(w);
+        void *const p_h = ptr<void>(h), *const p_y = ptr<void>(y);
+        uint8_t *const p_q = ptr<uint8_t>(q);
+        float *const p_s = ptr<float>(scale);
+        const int64_t ldx = ld(x), ldr = ld(r), ldh = ld(h), ldq = ld(q), lds = ld(scale), ldy = ld(y);
+        int rc;
+        {
+            Unlocked u;
+            rc = f_rmsnorm_fp8((uint32_t)batch, (uint64_t)n, p_x, xt, ldx, p_r, rt, ldr, p_h, ldh, p_w, wt, eps, p_q, ldq, p_s, lds, p_y,
+                               yt, ldy, st);
+        }
+        return PyLong_FromLong(rc);
+    });
+}
+
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, "addresses of the C functions"},
     {"decode", (PyCFunction)(void (*)(void))decode, METH_FASTCALL, "sqnn_decode"},
     {"matmul", (PyCFunction)(void (*)(void))matmul, METH_FASTCALL, "sqnn_decode_matmul"},
     {"matmul_static", (PyCFunction)(void (*)(void))matmul_static, METH_FASTCALL, "sqnn_decode_matmul_static"},
+    {"rmsnorm_fp8", (PyCFunction)(void (*)(void))rmsnorm_fp8, METH_FASTCALL, "sqnn_rmsnorm_fp8"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sqnn_python", "torch tensors to the C ABI of libsqnn", -1, methods,
                           nullptr, nullptr, nullptr, nullptr};

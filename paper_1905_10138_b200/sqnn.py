@@ -19,6 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("SQNN_LIBRARY") or os.path.join(_HERE, "libsqnn.so")
 
 MAX_PLANES = 8
+FP8_BLOCK = 128
 STATIC_SCRATCH_BYTES = 8 << 20
 OUT_BITS, OUT_BF16, OUT_SINK = 0, 1, 2
 X_F32, X_BF16 = 0, 1
@@ -123,6 +124,9 @@ def lib():
         L.sqnn_decode_matmul.argtypes = [P(Desc), vp, vp, vp, vp, i32, u32, i64, vp, i64, vp, sz, vp, vp]
         L.sqnn_decode_matmul_static.argtypes = [P(Desc), vp, vp, vp, vp, i32, u32, i64, vp, i64, vp, vp]
         L.sqnn_decode_matmul_static.restype = i32
+        L.sqnn_rmsnorm_fp8.argtypes = [u32, u64, vp, i32, i64, vp, i32, i64, vp, i64, vp, i32, ctypes.c_double, vp, i64, vp, i64, vp,
+                                       i32, i64, vp]
+        L.sqnn_rmsnorm_fp8.restype = i32
         L.sqnn_store_probe.argtypes = [vp, sz, u32, vp]
         L.sqnn_store_probe.restype = i32
         L.sqnn_set_debug_flags.argtypes = [u32, u64]
@@ -321,7 +325,7 @@ def _native():
         from . import _sqnn_python as mod
         L = lib()
         mod.bind(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value
-                   for f in ("sqnn_decode", "sqnn_decode_matmul", "sqnn_decode_matmul_static")))
+                   for f in ("sqnn_decode", "sqnn_decode_matmul", "sqnn_decode_matmul_static", "sqnn_rmsnorm_fp8")))
         _native_module = mod
     return _native_module
 
@@ -369,3 +373,13 @@ def sqnn_decode_matmul_static(desc: Desc, d_blob, d_mask, d_alpha, d_x, d_y, d_s
     status = (_native_module or _native()).matmul_static(desc, d_blob, d_mask, d_alpha, d_x, d_y, d_status, stream)
     if status:
         raise SqnnError(status, "sqnn_decode_matmul_static")
+
+
+def sqnn_rmsnorm_fp8(d_x, d_weight, eps: float, d_q, d_scale, d_residual=None, d_h=None, d_y=None, stream=None):
+    """h = d_x + d_residual (written to d_h; no residual: h = d_x), y = h / sqrt(mean(h^2) + eps) * d_weight, and of y its
+    8-bit form: d_q float8_e4m3fn [batch, n] with d_scale float32 [batch, ceil(n / 128)] (both may be None if only
+    d_y, y itself in float32 or bfloat16, is wanted).  d_x, d_residual and d_weight: float32 or bfloat16.
+    Queues on ``stream``; does not synchronise."""
+    status = (_native_module or _native()).rmsnorm_fp8(d_x, d_weight, eps, d_q, d_scale, d_residual, d_h, d_y, stream)
+    if status:
+        raise SqnnError(status, "sqnn_rmsnorm_fp8")
