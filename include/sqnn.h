@@ -344,7 +344,8 @@ int sqnn_store_probe(void *d_out, size_t bytes, uint32_t chunk_bytes, void *cuda
 
 /* For the library's own tests (the paper has no counterpart; not meant for applications).  Bit 0 of
  * `flags` makes the loader role of the tensor-core kernel for large batches issue no loads, bit 1 the MMA
- * role of the one for small batches report no completion, bit 2 the walk over care bits no bulk copies, so that the
+ * role of the one for small batches report no completion, bit 2 the walk over care bits no bulk copies, bit 3 the loader of the
+ * 8-bit product no loads, so that the
  * bounded waits of what comes after them run out: the kernel then reports 6 (= -SQNN_E_TIMEOUT)
  * through d_status, frees what it holds and returns; Y is left incomplete.  wait_limit_cycles is the number of SM clock cycles such a wait may
  * take (0 = the default, one to two seconds).  Applies to calls made
@@ -381,6 +382,21 @@ int sqnn_rmsnorm_fp8(uint32_t batch, uint64_t n, const void *d_x, int x_dtype, i
                      const void *d_weight, int weight_dtype, double eps,
                      uint8_t *d_q, int64_t ldq, float *d_scale, int64_t lds,
                      void *d_y, int y_dtype, int64_t ldy, void *cuda_stream);
+
+/* Product of an 8-bit layer: Y[b][r] = sum_c W[r][c] X[b][c] over the values the numbers stand for.
+ * d_w: m rows of n e4m3 numbers, row stride ldw; d_w_scale[ceil(m / 128)][ceil(n / 128)], row stride
+ * ldws.  d_x: batch rows of n, row stride ldx; d_x_scale[batch][ceil(n / 128)], row stride ldxs.  d_y:
+ * batch rows of m, row stride ldy, y_dtype SQNN_X_F32 or SQNN_X_BF16 (rounded once, at the end); fully
+ * overwritten, nothing beside the rows is touched.  Any m, n and batch from 1 on.  Sums are kept in fp32: over
+ * 128 columns in tensor memory, then scaled and added in registers, in a fixed order: results are bit-identical from run to
+ * run.  What is not finite goes through as in that sum.  One kernel, no workspace, nothing allocated.
+ * W and X need a 16-byte aligned base and row strides that are multiples of 16 (what lies between n and the
+ * stride is not used).  Errors: INVALID_ARG (NULL, sizes, strides, types), UNSUPPORTED (W or X
+ * not on 16-byte boundaries, m, n or batch above 2^30), CUDA; d_status as for the products. */
+int sqnn_fp8_matmul(uint64_t m, uint64_t n, uint32_t batch, const uint8_t *d_w, int64_t ldw,
+                    const float *d_w_scale, int64_t ldws, const uint8_t *d_x, int64_t ldx,
+                    const float *d_x_scale, int64_t ldxs, void *d_y, int y_dtype, int64_t ldy,
+                    uint32_t *d_status, void *cuda_stream);
 
 /* Scratch bytes sqnn_decode_matmul needs for this layer and batch (0 for batch <= 15). */
 size_t sqnn_workspace_bytes(const sqnn_desc *desc, uint32_t batch);

@@ -14,7 +14,7 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libsqnn.so")
 PY_MODULE = os.path.join(HERE, "_sqnn_python.so")
 PY_SOURCE = "sqnn_python.cpp"
-SOURCES = ["sqnn_host.cpp", "sqnn_api.cu", "sqnn_mma.cu", "sqnn_search.cu", "sqnn_norm.cu"]
+SOURCES = ["sqnn_host.cpp", "sqnn_api.cu", "sqnn_mma.cu", "sqnn_search.cu", "sqnn_norm.cu", "sqnn_fp8_mm.cu"]
 SHAPE_SOURCE = "sqnn_shape.cu"
 # (n_out, n_in) with compile-time kernels -- the list in csrc/sqnn_shapes.h -- plus the run-time shape (0, 0)
 SHAPES = [(40, 12), (40, 16), (60, 12), (80, 8), (80, 16), (100, 10), (200, 10), (0, 0)]

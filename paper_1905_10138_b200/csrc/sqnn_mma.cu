@@ -386,9 +386,7 @@ leave:
     if (warp == 4 * groups + 1) tmem_dealloc(tmem_base, 512);
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+}  // namespace
 
 EncodeTiledFn encode_tiled_fn()
 {
@@ -403,8 +401,6 @@ EncodeTiledFn encode_tiled_fn()
     }
     return fn;
 }
-
-}  // namespace
 
 DebugKnobs debug_knobs() { return DebugKnobs{g_debug_flags.load(), g_debug_wait_cycles.load()}; }
 

@@ -21,12 +21,13 @@ decltype(&sqnn_decode) f_decode = nullptr;
 decltype(&sqnn_decode_matmul) f_matmul = nullptr;
 decltype(&sqnn_decode_matmul_static) f_matmul_static = nullptr;
 decltype(&sqnn_rmsnorm_fp8) f_rmsnorm_fp8 = nullptr;
+decltype(&sqnn_fp8_matmul) f_fp8_matmul = nullptr;
 
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    if (nargs != 4) { PyErr_SetString(PyExc_TypeError, "bind takes four addresses"); return nullptr; }
-    void *p[4];
-    for (int i = 0; i < 4; ++i) {
+    if (nargs != 5) { PyErr_SetString(PyExc_TypeError, "bind takes five addresses"); return nullptr; }
+    void *p[5];
+    for (int i = 0; i < 5; ++i) {
         p[i] = PyLong_AsVoidPtr(args[i]);
         if (PyErr_Occurred()) return nullptr;
     }
@@ -34,6 +35,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     f_matmul = reinterpret_cast<decltype(f_matmul)>(p[1]);
     f_matmul_static = reinterpret_cast<decltype(f_matmul_static)>(p[2]);
     f_rmsnorm_fp8 = reinterpret_cast<decltype(f_rmsnorm_fp8)>(p[3]);
+    f_fp8_matmul = reinterpret_cast<decltype(f_fp8_matmul)>(p[4]);
     Py_RETURN_NONE;
 }
 
@@ -304,12 +306,56 @@ PyObject *rmsnorm_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs)
     });
 }
 
+bool status_word(const at::Tensor *t)
+{
+    if (!t) return true;
+    if (!on_device(t, "status")) return false;
+    return (t->numel() == 1 && t->element_size() == 4) || fail("status must be one 32-bit word");
+}
+
+// fp8_matmul(w, w_scale, x, x_scale, y, status, stream) -> status code
+PyObject *fp8_matmul(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return guarded([&]() -> PyObject * {
+        if (!enough(nargs, 7)) return nullptr;
+        const at::Tensor *w, *ws, *x, *xs, *y, *status;
+        void *st;
+        if (!tensor_arg(a[0], &w) || !tensor_arg(a[1], &ws) || !tensor_arg(a[2], &x) || !tensor_arg(a[3], &xs) || !tensor_arg(a[4], &y) ||
+            !tensor_arg(a[5], &status))
+            return nullptr;
+        if (!w || !ws || !x || !xs || !y) { fail("weights, activations, their scales and Y are required"); return nullptr; }
+        if (!matrix(w, -1, -1, "w")) return nullptr;
+        const int64_t m = w->size(0), n = w->size(1);
+        if (!matrix(x, -1, n, "x")) return nullptr;
+        const int64_t batch = x->size(0);
+        int yt;
+        if (!matrix(ws, blocks_of(m), blocks_of(n), "w_scale") || !matrix(xs, batch, blocks_of(n), "x_scale") || !matrix(y, batch, m, "y") ||
+            !of_type(w, at::kFloat8_e4m3fn, "w") || !of_type(x, at::kFloat8_e4m3fn, "x") || !of_type(ws, at::kFloat, "w_scale") ||
+            !of_type(xs, at::kFloat, "x_scale") || !real_type(y, &yt, "y") || !status_word(status))
+            return nullptr;
+        if (batch > 0x7fffffff) { fail("too many rows"); return nullptr; }
+        if (!stream_arg(a[6], &st)) return nullptr;
+        const uint8_t *const p_w = ptr<uint8_t>(w), *const p_x = ptr<uint8_t>(x);
+        const float *const p_ws = ptr<float>(ws), *const p_xs = ptr<float>(xs);
+        void *const p_y = ptr<void>(y);
+        uint32_t *const p_status = ptr<uint32_t>(status);
+        const int64_t ldw = row_stride(w), ldws = row_stride(ws), ldx = row_stride(x), ldxs = row_stride(xs), ldy = row_stride(y);
+        int rc;
+        {
+            Unlocked u;
+            rc = f_fp8_matmul((uint64_t)m, (uint64_t)n, (uint32_t)batch, p_w, ldw, p_ws, ldws, p_x, ldx, p_xs, ldxs, p_y, yt, ldy, p_status, st);
+        }
+        return PyLong_FromLong(rc);
+    });
+}
+
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, "addresses of the C functions"},
     {"decode", (PyCFunction)(void (*)(void))decode, METH_FASTCALL, "sqnn_decode"},
     {"matmul", (PyCFunction)(void (*)(void))matmul, METH_FASTCALL, "sqnn_decode_matmul"},
     {"matmul_static", (PyCFunction)(void (*)(void))matmul_static, METH_FASTCALL, "sqnn_decode_matmul_static"},
     {"rmsnorm_fp8", (PyCFunction)(void (*)(void))rmsnorm_fp8, METH_FASTCALL, "sqnn_rmsnorm_fp8"},
+    {"fp8_matmul", (PyCFunction)(void (*)(void))fp8_matmul, METH_FASTCALL, "sqnn_fp8_matmul"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sqnn_python", "torch tensors to the C ABI of libsqnn", -1, methods,
                           nullptr, nullptr, nullptr, nullptr};

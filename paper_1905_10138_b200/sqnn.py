@@ -127,6 +127,8 @@ def lib():
         L.sqnn_rmsnorm_fp8.argtypes = [u32, u64, vp, i32, i64, vp, i32, i64, vp, i64, vp, i32, ctypes.c_double, vp, i64, vp, i64, vp,
                                        i32, i64, vp]
         L.sqnn_rmsnorm_fp8.restype = i32
+        L.sqnn_fp8_matmul.argtypes = [u64, u64, u32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, i64, vp, vp]
+        L.sqnn_fp8_matmul.restype = i32
         L.sqnn_store_probe.argtypes = [vp, sz, u32, vp]
         L.sqnn_store_probe.restype = i32
         L.sqnn_set_debug_flags.argtypes = [u32, u64]
@@ -325,7 +327,8 @@ def _native():
         from . import _sqnn_python as mod
         L = lib()
         mod.bind(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value
-                   for f in ("sqnn_decode", "sqnn_decode_matmul", "sqnn_decode_matmul_static", "sqnn_rmsnorm_fp8")))
+                   for f in ("sqnn_decode", "sqnn_decode_matmul", "sqnn_decode_matmul_static", "sqnn_rmsnorm_fp8",
+                             "sqnn_fp8_matmul")))
         _native_module = mod
     return _native_module
 
@@ -346,7 +349,7 @@ def sqnn_store_probe(d_out, chunk_bytes: int = 3200, stream=None):
 
 def sqnn_set_debug_flags(flags: int, wait_limit_cycles: int = 0) -> None:
     """Test knob: bit 0 = the large-batch kernel's loader issues no loads, bit 1 = the small-batch kernel's MMA
-    warps report no completion, bit 2 = the walk over care bits issues no bulk copies; wait_limit_cycles bounds their waits."""
+    warps report no completion, bit 2 = the walk over care bits issues no bulk copies, bit 3 = the 8-bit product's loader issues no loads; wait_limit_cycles bounds their waits."""
     lib().sqnn_set_debug_flags(int(flags), int(wait_limit_cycles))
 
 
@@ -383,3 +386,13 @@ def sqnn_rmsnorm_fp8(d_x, d_weight, eps: float, d_q, d_scale, d_residual=None, d
     status = (_native_module or _native()).rmsnorm_fp8(d_x, d_weight, eps, d_q, d_scale, d_residual, d_h, d_y, stream)
     if status:
         raise SqnnError(status, "sqnn_rmsnorm_fp8")
+
+
+def sqnn_fp8_matmul(d_w, d_w_scale, d_x, d_x_scale, d_y, d_status=None, stream=None):
+    """Y[b, r] = sum_c W[r, c] X[b, c] of 8-bit weights and activations.  d_w: float8_e4m3fn [m, n] with d_w_scale float32
+    [ceil(m / 128), ceil(n / 128)]; d_x: float8_e4m3fn [batch, n] with d_x_scale float32 [batch, ceil(n / 128)] (as
+    ``sqnn_rmsnorm_fp8`` writes them); rows of both on 16-byte boundaries; d_y: [batch, m] float32 or bfloat16.
+    Queues on ``stream``; does not synchronise."""
+    status = (_native_module or _native()).fp8_matmul(d_w, d_w_scale, d_x, d_x_scale, d_y, d_status, stream)
+    if status:
+        raise SqnnError(status, "sqnn_fp8_matmul")
