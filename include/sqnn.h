@@ -398,6 +398,45 @@ int sqnn_fp8_matmul(uint64_t m, uint64_t n, uint32_t batch, const uint8_t *d_w, 
                     const float *d_x_scale, int64_t ldxs, void *d_y, int y_dtype, int64_t ldy,
                     uint32_t *d_status, void *cuda_stream);
 
+#define SQNN_MOE_MAX_TOKENS  64
+#define SQNN_MOE_MAX_EXPERTS 512
+#define SQNN_MOE_MAX_TOP_K   16
+#define SQNN_MOE_MAX_LOGITS  16384     /* tokens x experts */
+
+/* A mixture-of-experts layer in 8 bits.  router: experts rows of `hidden` elements (of the activations' type, row stride
+ * router_row).  gate_up: for each expert G then U, `inner` rows of `hidden` e4m3 numbers each (strides: gate_up_expert, gate_up_half from G to U,
+ * gate_up_row); gate_up_scale[experts][2][ceil(inner / 128)][ceil(hidden / 128)].  down: for each expert D, `hidden` rows of
+ * `inner` (strides down_expert, down_row); down_scale[experts][ceil(hidden / 128)][ceil(inner / 128)].  All device pointers.
+ * renormalize: shares are the softmax over the chosen experts (sum 1), else over all. */
+typedef struct sqnn_moe {
+    uint32_t experts, top_k, hidden, inner, renormalize, reserved;
+    const void *router;
+    const uint8_t *gate_up;
+    const float *gate_up_scale;
+    const uint8_t *down;
+    const float *down_scale;
+    int64_t router_row, gate_up_expert, gate_up_half, gate_up_row, down_expert, down_row;
+} sqnn_moe;
+
+/* The whole layer for a few tokens, router included: for each row x of d_x ([tokens][hidden], row stride ldx)
+ *   the top_k experts with the largest logits x . router[e] (equal ones: the lowest index) and their shares p
+ *   y = sum over them of p_e D_e (silu(G_e x) * (U_e x)),   silu(a) = a / (1 + exp(-a))
+ * to d_y ([tokens][hidden], row stride ldy, fully overwritten).  x_dtype (of d_x and router) and y_dtype:
+ * SQNN_X_F32 or SQNN_X_BF16.  Nothing is rounded to fewer than 22 bits on the way: logits are summed in 64 bits over eight products of fp32, all else
+ * in fp32; y is rounded to its type at the end.  Results are bit-identical from run to run.  A NaN among a token's logits counts as the
+ * largest, so the layer always has top_k different experts.  d_ids and d_probs ([tokens][top_k], may be NULL) get the
+ * experts, largest logit first, and their shares.  d_workspace: sqnn_moe_workspace_bytes bytes, 256-byte aligned, contents undefined
+ * before and after; calls that may run at the same time need one each.  Two kernels, nothing allocated.
+ * Weights need 16-byte aligned bases and strides that are multiples of 16; activations and router any.
+ * Errors: INVALID_ARG (NULL, sizes, strides, types, top_k above experts), UNSUPPORTED (tokens, experts, top_k or their products above the limits
+ * here, hidden or inner above 2^20, weights not on 16-byte boundaries), WORKSPACE, CUDA. */
+int sqnn_moe_fp8(const sqnn_moe *layer, uint32_t tokens, const void *d_x, int x_dtype, int64_t ldx,
+                 void *d_y, int y_dtype, int64_t ldy, int32_t *d_ids, float *d_probs,
+                 void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Scratch bytes sqnn_moe_fp8 needs (0 beyond its limits). */
+size_t sqnn_moe_workspace_bytes(uint32_t tokens, uint32_t top_k, uint32_t inner);
+
 /* Scratch bytes sqnn_decode_matmul needs for this layer and batch (0 for batch <= 15). */
 size_t sqnn_workspace_bytes(const sqnn_desc *desc, uint32_t batch);
 

@@ -1,0 +1,36 @@
+// Thread-block clusters: rank, barrier and the shared memory of the other blocks.
+#pragma once
+#include "sqnn_decode.cuh"
+
+namespace sqnn {
+
+SQNN_DEV uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(r)); return r; }
+SQNN_DEV void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
+SQNN_DEV uint32_t peer_addr(uint32_t sa, uint32_t rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(sa), "r"(rank));
+    return a;
+}
+SQNN_DEV float4 peer_load4(uint32_t a)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+SQNN_DEV uint32_t peer_load(uint32_t a)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+
+SQNN_DEV void peer_store(uint32_t a, double v)
+{
+    asm volatile("st.shared::cluster.f64 [%0], %1;\n" :: "r"(a), "d"(v) : "memory");
+}
+
+}  // namespace sqnn

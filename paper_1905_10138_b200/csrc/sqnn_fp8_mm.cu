@@ -14,6 +14,7 @@
 // distributed shared memory in the order of their rank.  No workspace, no atomics: results are the same from run to run.
 #include "sqnn_launch.h"
 #include "sqnn_fp8.cuh"
+#include "sqnn_cluster.cuh"
 #include "sqnn_tc.cuh"
 
 #include <cuda_bf16.h>
@@ -61,30 +62,6 @@ SQNN_DEV void mma_block(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_
 }
 // Instruction descriptor: D fp32, A and B e4m3, both K-major, M = 128, N = n.
 SQNN_DEV uint32_t instr_desc_fp8(uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
-
-SQNN_DEV uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(r)); return r; }
-SQNN_DEV void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-}
-SQNN_DEV uint32_t peer_addr(uint32_t sa, uint32_t rank)
-{
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(sa), "r"(rank));
-    return a;
-}
-SQNN_DEV float4 peer_load4(uint32_t a)
-{
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
-    return v;
-}
-SQNN_DEV uint32_t peer_load(uint32_t a)
-{
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
 
 // acc (two fp32 numbers) += t * s
 SQNN_DEV void fma2(uint64_t &acc, uint32_t lo, uint32_t hi, uint64_t s)

@@ -22,12 +22,13 @@ decltype(&sqnn_decode_matmul) f_matmul = nullptr;
 decltype(&sqnn_decode_matmul_static) f_matmul_static = nullptr;
 decltype(&sqnn_rmsnorm_fp8) f_rmsnorm_fp8 = nullptr;
 decltype(&sqnn_fp8_matmul) f_fp8_matmul = nullptr;
+decltype(&sqnn_moe_fp8) f_moe_fp8 = nullptr;
 
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    if (nargs != 5) { PyErr_SetString(PyExc_TypeError, "bind takes five addresses"); return nullptr; }
-    void *p[5];
-    for (int i = 0; i < 5; ++i) {
+    if (nargs != 6) { PyErr_SetString(PyExc_TypeError, "bind takes six addresses"); return nullptr; }
+    void *p[6];
+    for (int i = 0; i < 6; ++i) {
         p[i] = PyLong_AsVoidPtr(args[i]);
         if (PyErr_Occurred()) return nullptr;
     }
@@ -36,6 +37,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     f_matmul_static = reinterpret_cast<decltype(f_matmul_static)>(p[2]);
     f_rmsnorm_fp8 = reinterpret_cast<decltype(f_rmsnorm_fp8)>(p[3]);
     f_fp8_matmul = reinterpret_cast<decltype(f_fp8_matmul)>(p[4]);
+    f_moe_fp8 = reinterpret_cast<decltype(f_moe_fp8)>(p[5]);
     Py_RETURN_NONE;
 }
 
@@ -349,6 +351,85 @@ PyObject *fp8_matmul(PyObject *, PyObject *const *a, Py_ssize_t nargs)
     });
 }
 
+// moe_fp8(x, router, top_k, renormalize, gate_up, gate_up_scale, down, down_scale, y, workspace, ids, probs, stream) -> status code
+PyObject *moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return guarded([&]() -> PyObject * {
+        if (!enough(nargs, 13)) return nullptr;
+        const at::Tensor *x, *router, *gu, *gus, *down, *downs, *y, *ws, *ids, *probs;
+        void *st;
+        if (!tensor_arg(a[0], &x) || !tensor_arg(a[1], &router) || !tensor_arg(a[4], &gu) || !tensor_arg(a[5], &gus) || !tensor_arg(a[6], &down) ||
+            !tensor_arg(a[7], &downs) || !tensor_arg(a[8], &y) || !tensor_arg(a[9], &ws) || !tensor_arg(a[10], &ids) || !tensor_arg(a[11], &probs))
+            return nullptr;
+        const long top_k = PyLong_AsLong(a[2]);
+        if (top_k == -1 && PyErr_Occurred()) return nullptr;
+        const int renormalize = PyObject_IsTrue(a[3]);
+        if (renormalize < 0) return nullptr;
+        if (!x || !router || !gu || !gus || !down || !downs || !y) { fail("x, router, weights, their scales and y are required"); return nullptr; }
+        if (!matrix(x, -1, -1, "x")) return nullptr;
+        const int64_t tokens = x->size(0), hidden = x->size(1);
+        if (!matrix(router, -1, hidden, "router") || !matrix(y, tokens, hidden, "y")) return nullptr;
+        const int64_t experts = router->size(0);
+        int xt, rt, yt;
+        if (!real_type(x, &xt, "x") || !real_type(router, &rt, "router") || !real_type(y, &yt, "y")) return nullptr;
+        if (xt != rt) { fail("router must be of x's type"); return nullptr; }
+        if (!on_device(gu, "gate_up") || !on_device(gus, "gate_up_scale") || !on_device(down, "down") || !on_device(downs, "down_scale") ||
+            !on_device(ws, "workspace") || !on_device(ids, "ids") || !on_device(probs, "probs") || !of_type(gu, at::kFloat8_e4m3fn, "gate_up") ||
+            !of_type(down, at::kFloat8_e4m3fn, "down") || !of_type(gus, at::kFloat, "gate_up_scale") || !of_type(downs, at::kFloat, "down_scale"))
+            return nullptr;
+        if (gu->dim() != 4 || gu->size(0) != experts || gu->size(1) != 2 || gu->size(3) != hidden || (hidden > 1 && gu->stride(3) != 1)) {
+            fail("gate_up must be [experts, 2, inner, hidden] with unit inner stride");
+            return nullptr;
+        }
+        const int64_t inner = gu->size(2);
+        if (down->dim() != 3 || down->size(0) != experts || down->size(1) != hidden || down->size(2) != inner || (inner > 1 && down->stride(2) != 1)) {
+            fail("down must be [experts, hidden, inner] with unit inner stride");
+            return nullptr;
+        }
+        const int64_t gus_shape[4] = {experts, 2, blocks_of(inner), blocks_of(hidden)}, downs_shape[3] = {experts, blocks_of(hidden), blocks_of(inner)};
+        if (gus->sizes() != at::IntArrayRef(gus_shape, 4) || !gus->is_contiguous() || downs->sizes() != at::IntArrayRef(downs_shape, 3) || !downs->is_contiguous()) {
+            fail("scales must be contiguous, one per 128 x 128 block");
+            return nullptr;
+        }
+        const int64_t pair_shape[2] = {tokens, top_k};
+        if (ids && (ids->scalar_type() != at::kInt || ids->sizes() != at::IntArrayRef(pair_shape, 2) || !ids->is_contiguous())) {
+            fail("ids must be contiguous int32 [tokens, top_k]");
+            return nullptr;
+        }
+        if (probs && (probs->scalar_type() != at::kFloat || probs->sizes() != at::IntArrayRef(pair_shape, 2) || !probs->is_contiguous())) {
+            fail("probs must be contiguous float32 [tokens, top_k]");
+            return nullptr;
+        }
+        if (ws && !ws->is_contiguous()) { fail("workspace must be contiguous"); return nullptr; }
+        const int64_t most = 1ll << 31;
+        if (tokens >= most || experts >= most || top_k < 0 || top_k >= most || hidden >= most || inner >= most) { fail("too large"); return nullptr; }
+        if (!stream_arg(a[12], &st)) return nullptr;
+        // the stride of a dimension of one element is whatever torch says: 0 suits every check
+        const auto stride = [](const at::Tensor *t, int64_t d, int64_t one) { return t->size(d) == 1 ? one : t->stride(d); };
+        sqnn_moe L = {};
+        L.experts = (uint32_t)experts; L.top_k = (uint32_t)top_k; L.hidden = (uint32_t)hidden; L.inner = (uint32_t)inner;
+        L.renormalize = (uint32_t)renormalize;
+        L.router = ptr<void>(router);
+        L.gate_up = ptr<uint8_t>(gu); L.gate_up_scale = ptr<float>(gus);
+        L.down = ptr<uint8_t>(down); L.down_scale = ptr<float>(downs);
+        L.router_row = row_stride(router);
+        L.gate_up_expert = stride(gu, 0, 0); L.gate_up_half = gu->stride(1); L.gate_up_row = stride(gu, 2, (hidden + 15) / 16 * 16);
+        L.down_expert = stride(down, 0, 0); L.down_row = stride(down, 1, (inner + 15) / 16 * 16);
+        const void *const p_x = ptr<void>(x);
+        void *const p_y = ptr<void>(y), *const p_ws = ptr<void>(ws);
+        int32_t *const p_ids = ptr<int32_t>(ids);
+        float *const p_probs = ptr<float>(probs);
+        const int64_t ldx = row_stride(x), ldy = row_stride(y);
+        const size_t ws_bytes = bytes_of(ws);
+        int rc;
+        {
+            Unlocked u;
+            rc = f_moe_fp8(&L, (uint32_t)tokens, p_x, xt, ldx, p_y, yt, ldy, p_ids, p_probs, p_ws, ws_bytes, st);
+        }
+        return PyLong_FromLong(rc);
+    });
+}
+
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, "addresses of the C functions"},
     {"decode", (PyCFunction)(void (*)(void))decode, METH_FASTCALL, "sqnn_decode"},
@@ -356,6 +437,7 @@ PyMethodDef methods[] = {
     {"matmul_static", (PyCFunction)(void (*)(void))matmul_static, METH_FASTCALL, "sqnn_decode_matmul_static"},
     {"rmsnorm_fp8", (PyCFunction)(void (*)(void))rmsnorm_fp8, METH_FASTCALL, "sqnn_rmsnorm_fp8"},
     {"fp8_matmul", (PyCFunction)(void (*)(void))fp8_matmul, METH_FASTCALL, "sqnn_fp8_matmul"},
+    {"moe_fp8", (PyCFunction)(void (*)(void))moe_fp8, METH_FASTCALL, "sqnn_moe_fp8"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sqnn_python", "torch tensors to the C ABI of libsqnn", -1, methods,
                           nullptr, nullptr, nullptr, nullptr};

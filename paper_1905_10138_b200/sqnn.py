@@ -20,6 +20,7 @@ LIB_PATH = os.environ.get("SQNN_LIBRARY") or os.path.join(_HERE, "libsqnn.so")
 
 MAX_PLANES = 8
 FP8_BLOCK = 128
+MOE_MAX_TOKENS, MOE_MAX_EXPERTS, MOE_MAX_TOP_K, MOE_MAX_LOGITS = 64, 512, 16, 16384
 STATIC_SCRATCH_BYTES = 8 << 20
 OUT_BITS, OUT_BF16, OUT_SINK = 0, 1, 2
 X_F32, X_BF16 = 0, 1
@@ -85,6 +86,12 @@ class Desc(ctypes.Structure):
                 ("n_pp", ctypes.c_uint64 * MAX_PLANES), ("total_bytes", ctypes.c_uint64)]
 
 
+class Moe(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_uint32) for f in ("experts", "top_k", "hidden", "inner", "renormalize", "reserved")] + \
+               [(f, ctypes.c_void_p) for f in ("router", "gate_up", "gate_up_scale", "down", "down_scale")] + \
+               [(f, ctypes.c_int64) for f in ("router_row", "gate_up_expert", "gate_up_half", "gate_up_row", "down_expert", "down_row")]
+
+
 _lib = None
 
 
@@ -129,6 +136,10 @@ def lib():
         L.sqnn_rmsnorm_fp8.restype = i32
         L.sqnn_fp8_matmul.argtypes = [u64, u64, u32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, i64, vp, vp]
         L.sqnn_fp8_matmul.restype = i32
+        L.sqnn_moe_fp8.argtypes = [P(Moe), u32, vp, i32, i64, vp, i32, i64, vp, vp, vp, sz, vp]
+        L.sqnn_moe_fp8.restype = i32
+        L.sqnn_moe_workspace_bytes.argtypes = [u32, u32, u32]
+        L.sqnn_moe_workspace_bytes.restype = sz
         L.sqnn_store_probe.argtypes = [vp, sz, u32, vp]
         L.sqnn_store_probe.restype = i32
         L.sqnn_set_debug_flags.argtypes = [u32, u64]
@@ -328,7 +339,7 @@ def _native():
         L = lib()
         mod.bind(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value
                    for f in ("sqnn_decode", "sqnn_decode_matmul", "sqnn_decode_matmul_static", "sqnn_rmsnorm_fp8",
-                             "sqnn_fp8_matmul")))
+                             "sqnn_fp8_matmul", "sqnn_moe_fp8")))
         _native_module = mod
     return _native_module
 
@@ -396,3 +407,22 @@ def sqnn_fp8_matmul(d_w, d_w_scale, d_x, d_x_scale, d_y, d_status=None, stream=N
     status = (_native_module or _native()).fp8_matmul(d_w, d_w_scale, d_x, d_x_scale, d_y, d_status, stream)
     if status:
         raise SqnnError(status, "sqnn_fp8_matmul")
+
+
+def sqnn_moe_workspace_bytes(tokens: int, top_k: int, inner: int) -> int:
+    return int(lib().sqnn_moe_workspace_bytes(int(tokens), int(top_k), int(inner)))
+
+
+def sqnn_moe_fp8(d_x, d_router, top_k: int, renormalize: bool, d_gate_up, d_gate_up_scale, d_down, d_down_scale, d_y, d_workspace,
+                 d_ids=None, d_probs=None, stream=None):
+    """A mixture-of-experts layer for up to ``MOE_MAX_TOKENS`` tokens: the ``top_k`` experts with the largest d_x . d_router (equal ones:
+    the lowest index), and y = sum of their shares times D (silu(G x) * (U x)).  d_x: [tokens, hidden] and d_router: [experts, hidden],
+    float32 or bfloat16 alike; d_gate_up: float8_e4m3fn [experts, 2, inner, hidden] (G, then U) with d_gate_up_scale float32
+    [experts, 2, ceil(inner / 128), ceil(hidden / 128)]; d_down: float8_e4m3fn [experts, hidden, inner] with d_down_scale float32
+    [experts, ceil(hidden / 128), ceil(inner / 128)]; rows of the weights on 16-byte boundaries; d_y: [tokens, hidden] float32 or bfloat16;
+    d_workspace: ``sqnn_moe_workspace_bytes`` bytes; d_ids int32 and d_probs float32 [tokens, top_k] get the choice (may be None).
+    ``renormalize``: the shares of the chosen experts sum to 1.  Queues on ``stream``; does not synchronise."""
+    status = (_native_module or _native()).moe_fp8(d_x, d_router, top_k, renormalize, d_gate_up, d_gate_up_scale, d_down, d_down_scale, d_y,
+                                                   d_workspace, d_ids, d_probs, stream)
+    if status:
+        raise SqnnError(status, "sqnn_moe_fp8")
