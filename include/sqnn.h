@@ -345,7 +345,7 @@ int sqnn_store_probe(void *d_out, size_t bytes, uint32_t chunk_bytes, void *cuda
 /* For the library's own tests (the paper has no counterpart; not meant for applications).  Bit 0 of
  * `flags` makes the loader role of the tensor-core kernel for large batches issue no loads, bit 1 the MMA
  * role of the one for small batches report no completion, bit 2 the walk over care bits no bulk copies, bit 3 the loader of the
- * 8-bit product no loads, so that the
+ * 8-bit product no loads, bit 4 those of the mixture-of-experts layer, so that the
  * bounded waits of what comes after them run out: the kernel then reports 6 (= -SQNN_E_TIMEOUT)
  * through d_status, frees what it holds and returns; Y is left incomplete.  wait_limit_cycles is the number of SM clock cycles such a wait may
  * take (0 = the default, one to two seconds).  Applies to calls made
@@ -402,6 +402,7 @@ int sqnn_fp8_matmul(uint64_t m, uint64_t n, uint32_t batch, const uint8_t *d_w, 
 #define SQNN_MOE_MAX_EXPERTS 512
 #define SQNN_MOE_MAX_TOP_K   16
 #define SQNN_MOE_MAX_LOGITS  16384     /* tokens x experts */
+#define SQNN_MOE_MAX_WIDTH   14336     /* hidden, inner    */
 
 /* A mixture-of-experts layer in 8 bits.  router: experts rows of `hidden` elements (of the activations' type, row stride
  * router_row).  gate_up: for each expert G then U, `inner` rows of `hidden` e4m3 numbers each (strides: gate_up_expert, gate_up_half from G to U,
@@ -427,12 +428,13 @@ typedef struct sqnn_moe {
  * largest, so the layer always has top_k different experts.  d_ids and d_probs ([tokens][top_k], may be NULL) get the
  * experts, largest logit first, and their shares.  d_workspace: sqnn_moe_workspace_bytes bytes, 256-byte aligned, contents undefined
  * before and after; calls that may run at the same time need one each.  Two kernels, nothing allocated.
- * Weights need 16-byte aligned bases and strides that are multiples of 16; activations and router any.
+ * Weights need 16-byte aligned bases, row strides that are multiples of 16 and expert and half strides that are multiples of the
+ * row stride; activations and router any.  d_status as for the products.
  * Errors: INVALID_ARG (NULL, sizes, strides, types, top_k above experts), UNSUPPORTED (tokens, experts, top_k or their products above the limits
- * here, hidden or inner above 2^20, weights not on 16-byte boundaries), WORKSPACE, CUDA. */
+ * here, hidden or inner above SQNN_MOE_MAX_WIDTH, weights not on 16-byte boundaries), WORKSPACE, CUDA. */
 int sqnn_moe_fp8(const sqnn_moe *layer, uint32_t tokens, const void *d_x, int x_dtype, int64_t ldx,
                  void *d_y, int y_dtype, int64_t ldy, int32_t *d_ids, float *d_probs,
-                 void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+                 void *d_workspace, size_t workspace_bytes, uint32_t *d_status, void *cuda_stream);
 
 /* Scratch bytes sqnn_moe_fp8 needs (0 beyond its limits). */
 size_t sqnn_moe_workspace_bytes(uint32_t tokens, uint32_t top_k, uint32_t inner);

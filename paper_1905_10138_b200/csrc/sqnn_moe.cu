@@ -4,23 +4,29 @@
 //   y = sum over a token's experts e of p_e D_e (silu(G_e x) * (U_e x)),    silu(a) = a / (1 + exp(-a))
 //
 // Few tokens reach many experts, so nearly every weight is used for one or two tokens: the layer is bound by reading the chosen experts'
-// weights once.  They go from global memory to registers (a warp keeps several 16-byte loads per lane in flight), become fp16 there (exact)
-// and are the A operand of mma.sync m16n8k16: 16 rows by 16 columns, up to eight tokens as the columns of B.  (mma.sync, not tcgen05: a
-// stage in shared memory would only add a step to a stream that is used once, and the rate of mma.sync is several times what memory asks for.)
-// The columns of a chunk of 64 are dealt to the MMAs so that a lane's 16 bytes of a row are its share of four of them.
+// weights once.  A warp takes 16 rows (or twice 16) by 128 columns at a time: one lane has TMA copy them into the warp's own ring in shared memory,
+// several steps ahead; ldmatrix gives every lane four neighbouring bytes of a row, they become fp16 (exact) and are the A operand
+// of mma.sync m16n8k16 with up to eight tokens as the columns of B.  (mma.sync, not tcgen05: weights that are used once gain nothing
+// from a tile that many warps share, and the rate of mma.sync is several times what memory asks for.  Weights read straight into registers, 62 us
+// for one token and 8 of 64 experts of 2048 x 1024: the unrolled code did not fit the instruction cache.  A ring filled by 16-byte copies of
+// every lane, 38 us: 230 to 280 instructions per kilobyte or two, most of them addresses.  This form: @T1@.)
+// The 16 columns of an MMA are dealt so that its k slots 2 t, 2 t + 1, 2 t + 8, 2 t + 9 are columns 4 t .. 4 t + 3, and B is stored
+// in the order that gives a lane its share of four MMAs in 32 bytes: position 16 t + 4 j + i of 64 holds column 16 j + 4 t + i.
 //
-// Activations are scaled by a power of two per chunk of 64 columns and token so that the largest lies below 2^15, and cut into fp16
-// pieces: bf16 numbers are exact in one (down to 2^-40 of the chunk's largest), fp32 numbers leave 2^-22 with two.  Sums are fp32, per chunk in the MMA, then
-// scaled by the weights' and the activations' scale and added to 32-bit sums.
+// Activations are scaled by a power of two so that the largest lies below 2^15, and cut into fp16 pieces: bf16 numbers are exact in
+// one, fp32 numbers keep 22 bits in two (both down to 2^-40 of the largest).  x is scaled per token, the inner values, whose
+// largest nobody knows before all are there, per token and MMA: a unit of the first kernel is the 16 inner values of one MMA of the second.
+// Sums are fp32 in the MMA, then scaled and added to 32-bit sums.
 //
 // k_moe_up:   every cluster works out the routing for itself (its CTAs share the experts' logits through distributed shared memory), then the CTAs
-//             share all (expert, 8 rows of G and the same 8 of U); a CTA's warps share the columns of up to 16 such units at a time.
-// k_moe_down: a CTA has 16 rows of all chosen experts' D; its warps share (expert, chunk of columns) evenly; each sums into its own
+//             share all units (expert, 16 rows of G and the same of U); a CTA's warps share the columns of up to 16 units at a time.
+// k_moe_down: a CTA has 16 or 32 rows of all chosen experts' D; its warps share (expert, 128 columns) evenly; each sums into its own
 //             accumulators, which are added up in warp order.
 // No atomics on sums: results are the same from run to run.
 #include "sqnn_launch.h"
 #include "sqnn_fp8.cuh"
 #include "sqnn_cluster.cuh"
+#include "sqnn_tc.cuh"
 
 #include <cuda_bf16.h>
 
@@ -29,28 +35,51 @@
 namespace sqnn {
 namespace {
 
-constexpr uint32_t WARPS = 16, THREADS = WARPS * 32;
+constexpr uint32_t WARPS = 16, THREADS = WARPS * 32;              // first kernel; the second has STREAMS warps
+constexpr uint32_t STREAMS = 8;           // warps that stream weights
 constexpr uint32_t CLUSTER = 4;           // CTAs that share the routing's work
-constexpr uint32_t CHUNK = 64;            // columns per step of a warp
-constexpr uint32_t AHEAD = 6;             // steps whose weights are in flight
+constexpr uint32_t STEP = FP8_BLOCK;      // columns per step of a warp
+constexpr uint32_t GROUP = 8;             // tokens multiplied together
 constexpr uint32_t MAX_TOKENS = SQNN_MOE_MAX_TOKENS, MAX_EXPERTS = SQNN_MOE_MAX_EXPERTS, MAX_TOP_K = SQNN_MOE_MAX_TOP_K;
 constexpr uint32_t MAX_PAIRS = MAX_TOKENS * MAX_TOP_K;
-constexpr uint32_t MAX_ENTRIES = MAX_EXPERTS + MAX_PAIRS / 8;     // chosen experts, those with many tokens several times
+constexpr uint32_t MAX_ENTRIES = MAX_EXPERTS + MAX_PAIRS;         // chosen experts, those with many tokens several times
+constexpr size_t SMEM_BYTES = 224 * 1024;
+constexpr uint32_t UP_DEPTH = 4, UP_SLOT = 2 * 16 * STEP;         // first kernel's ring: 16 rows of G and of U
+constexpr uint32_t PARTS_BYTES = STREAMS * 2 * 8 * 32 * 4;        // [warp][its first or second unit][sum][lane]
+constexpr uint32_t H_BLOCK = 2 * 2 * STEP + 4 * (STEP / 16);      // inner values of a token, 128 columns: two pieces and eight scales
+constexpr uint32_t H_PITCH = H_BLOCK + 16;                        // the same in shared memory: neighbouring tokens in other banks
+constexpr uint32_t MAX_DOWN_DEPTH = 8;
+constexpr uint64_t WAIT_LIMIT_CYCLES = 4000000000ull;
+
+// An entry of the list of chosen experts, as the second kernel needs it.
+struct Entry {
+    uint32_t expert, count;               // count <= GROUP tokens
+    uint32_t token[GROUP];
+    uint32_t pair[GROUP];                 // rows of h
+    float prob[GROUP];
+};
 
 struct MoeArgs {
     const void *x, *router;
     const uint8_t *gate_up, *down;
     const float *gate_up_scale, *down_scale;
     void *y;
-    float *h;                     // workspace: [tokens * top_k][pitch]
-    int32_t *ids;                 // workspace: [tokens * top_k]
-    float *probs;
+    uint8_t *h;                   // workspace: a row of blocks per (token, choice)
+    Entry *list;                  // workspace
+    uint32_t *list_size;
     int32_t *ids_out;
     float *probs_out;
     int64_t ldx, ldr, ldy;
-    int64_t gu_expert, gu_half, gu_row, d_expert, d_row;          // strides
-    uint32_t tokens, experts, top_k, hidden, inner, pitch;
+    uint32_t gu_expert, gu_half, d_expert;                        // in rows
+    uint32_t tokens, experts, top_k, hidden, inner;
+    uint32_t h_row;               // bytes per row of h
     uint32_t renormalize, x_vec, r_vec, y_bf16;
+    uint32_t x_row, x_rows;       // first kernel: bytes per staged row of x, how many there is room for
+    uint32_t per;                 // tokens per entry in the first kernel
+    uint32_t depth, slot;         // second kernel's ring
+    uint32_t skip_loads;          // test only: no weights are asked for
+    uint64_t wait_limit;
+    uint32_t *status;
 };
 
 // ---- routing tables in shared memory
@@ -62,6 +91,7 @@ struct Routing {
     uint32_t entry[MAX_ENTRIES];          // expert | group of tokens << 16
     uint32_t totals[WARPS];
     uint32_t entries;
+    uint32_t exponent[MAX_TOKENS];        // biased, of a token's largest activation
 };
 constexpr uint32_t ROUTING_BYTES = (sizeof(Routing) + 127) / 128 * 128;
 
@@ -96,6 +126,7 @@ SQNN_DEV void list_entries(Routing &R, const MoeArgs &M, uint32_t per)
     if (tid == 0) R.entries = all;
     __syncthreads();
 }
+SQNN_DEV uint32_t tokens_of(const Routing &R, uint32_t expert) { return __popc(R.mask[expert][0]) + __popc(R.mask[expert][1]); }
 // The n-th token of an expert, MAX_TOKENS if it has fewer.
 SQNN_DEV uint32_t token_of(const Routing &R, uint32_t expert, uint32_t n)
 {
@@ -112,57 +143,6 @@ SQNN_DEV uint32_t pair_of(const Routing &R, const MoeArgs &M, uint32_t token, ui
     uint32_t s = 0;
     while (s + 1 < M.top_k && R.ids[token * M.top_k + s] != (int32_t)expert) ++s;
     return token * M.top_k + s;
-}
-
-// ---- loads
-
-SQNN_DEV uint4 stream16(const uint8_t *p)
-{
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
-// 16 bytes of a row from byte `at` on; bytes from `n` on are zero (rows start on 16-byte boundaries, but the last may end with its data).
-SQNN_DEV uint4 row16(const uint8_t *row, uint32_t at, uint32_t n)
-{
-    if (at + 16 <= n) return stream16(row + at);
-    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (uint32_t j = 0; j < 16; ++j)
-        if (at + j < n) w[j >> 2] |= (uint32_t)row[at + j] << (8 * (j & 3));
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-// 16 elements of a row of activations from element `at` on as fp32; elements from `n` on are zero.
-SQNN_DEV void values16(const float *row, uint32_t at, uint32_t n, bool vec, float (&v)[16])
-{
-    if (vec && at + 16 <= n) {
-#pragma unroll
-        for (uint32_t j = 0; j < 16; j += 4) {
-            const float4 f = *reinterpret_cast<const float4 *>(row + at + j);
-            v[j] = f.x; v[j + 1] = f.y; v[j + 2] = f.z; v[j + 3] = f.w;
-        }
-    } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 16; ++j) v[j] = at + j < n ? row[at + j] : 0.0f;
-    }
-}
-SQNN_DEV void values16(const __nv_bfloat16 *row, uint32_t at, uint32_t n, bool vec, float (&v)[16])
-{
-    if (vec && at + 16 <= n) {
-#pragma unroll
-        for (uint32_t j = 0; j < 16; j += 8) {
-            const uint4 f = *reinterpret_cast<const uint4 *>(row + at + j);
-            const uint32_t u[4] = {f.x, f.y, f.z, f.w};
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) {
-                v[j + 2 * i] = __uint_as_float(u[i] << 16);
-                v[j + 2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-            }
-        }
-    } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 16; ++j) v[j] = at + j < n ? __bfloat162float(row[at + j]) : 0.0f;
-    }
 }
 
 // ---- the multiplication of one chunk
@@ -187,41 +167,46 @@ SQNN_DEV void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// B operand of a chunk: this lane's 16 columns of its token (lane / 4), in one or two pieces.
-template <bool EXACT16>
-struct Columns {
-    uint32_t hi[8], lo[EXACT16 ? 1 : 8];
-    float back;                   // what undoes the scaling
-    SQNN_DEV void make(const float (&v)[16])
-    {
-        uint32_t top = 0;
-#pragma unroll
-        for (uint32_t j = 0; j < 16; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const uint32_t e = max(top >> 23, 15u);                  // 255 for infinities and NaN: finite numbers stay finite beside them
-        const float s = __uint_as_float((268u - e) << 23);       // 2^(14 - (e - 127))
-        back = __uint_as_float((e - 14u) << 23);
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-            const float a = v[2 * j] * s, b = v[2 * j + 1] * s;
-            hi[j] = f16x2(a, b);
-            if constexpr (!EXACT16) lo[j] = f16x2(a - f16_lo(hi[j]), b - f16_hi(hi[j]));
-        }
-    }
-};
+// The power of two that brings a magnitude of this biased exponent below 2^15, and its inverse.  (255, infinities and NaN: finite numbers stay finite
+// beside them.)
+SQNN_DEV uint32_t exponent_of(uint32_t magnitude) { return max(magnitude >> 23, 15u); }
+SQNN_DEV float scale_of(uint32_t e) { return __uint_as_float((268u - e) << 23); }       // 2^(14 - (e - 127))
+SQNN_DEV float back_of(uint32_t e) { return __uint_as_float((e - 14u) << 23); }
 
-// c += (16 rows x 64 columns of weights) . B
-template <bool EXACT16>
-SQNN_DEV void multiply(float (&c)[4], const uint4 &top, const uint4 &bottom, const Columns<EXACT16> &B)
+SQNN_DEV void bulk_load(uint32_t sdst, const void *src, uint32_t bytes, uint32_t bar)
 {
-    const uint32_t r[4] = {top.x, top.y, top.z, top.w}, q[4] = {bottom.x, bottom.y, bottom.z, bottom.w};
-#pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) {
-        const uint32_t a[4] = {fp8x2_to_f16x2(r[j]), fp8x2_to_f16x2(q[j]), fp8x2_to_f16x2(r[j] >> 16), fp8x2_to_f16x2(q[j] >> 16)};
-        mma_f16(c, a, B.hi[2 * j], B.hi[2 * j + 1]);
-        if constexpr (!EXACT16) mma_f16(c, a, B.lo[2 * j], B.lo[2 * j + 1]);
-    }
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n"
+                 :: "r"(sdst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+SQNN_DEV uint4 shared16(uint32_t sa)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(sa) : "memory");
+    return v;
+}
+SQNN_DEV float shared4(uint32_t sa)
+{
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v) : "r"(sa) : "memory");
+    return v;
+}
+// Four 8 x 16-byte matrices: lane 8 i + r gives the address of row r of matrix i and gets bytes 4 (lane % 4) .. + 3 of row lane / 4 of each.
+SQNN_DEV uint4 matrices(uint32_t sa)
+{
+    uint4 v;
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(sa) : "memory");
+    return v;
+}
+// Where a lane's row for matrices() lies in a tile of 16 rows by 128 bytes with the 128-byte swizzle (on a 1024-byte boundary): matrices of rows 0 - 7 and 8 - 15
+// of 16 columns, then of the next 16; `^ (p << 5)` for columns 32 p on.
+SQNN_DEV uint32_t matrix_row(uint32_t lane) { return ((lane & 7) + (lane & 8)) * STEP + (((lane >> 4) ^ (lane & 7)) << 4); }
+// A operand of an MMA from a lane's four bytes of row g and of row g + 8.
+SQNN_DEV void weights_of(uint32_t (&a)[4], uint32_t top, uint32_t bottom)
+{
+    a[0] = fp8x2_to_f16x2(top);
+    a[1] = fp8x2_to_f16x2(bottom);
+    a[2] = fp8x2_to_f16x2(top >> 16);
+    a[3] = fp8x2_to_f16x2(bottom >> 16);
 }
 
 // ---- routing
@@ -258,17 +243,17 @@ template <typename XT>
 SQNN_DEV void logits_of_cluster(const MoeArgs &M, double *logits)
 {
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = cluster_rank();
-    constexpr uint32_t GROUP = 4;                                // tokens that share a read of an expert's row
-    const uint32_t groups = (M.tokens + GROUP - 1) / GROUP, mine = (M.experts - rank + CLUSTER - 1) / CLUSTER;
+    constexpr uint32_t SHARE = 4;                                // tokens that share a read of an expert's row
+    const uint32_t groups = (M.tokens + SHARE - 1) / SHARE, mine = (M.experts - rank + CLUSTER - 1) / CLUSTER;
     const XT *const x = static_cast<const XT *>(M.x), *const router = static_cast<const XT *>(M.router);
     for (uint32_t i = warp; i < mine * groups; i += WARPS) {
-        const uint32_t e = rank + CLUSTER * (i / groups), t0 = i % groups * GROUP;
-        double sum[GROUP] = {};
+        const uint32_t e = rank + CLUSTER * (i / groups), t0 = i % groups * SHARE;
+        double sum[SHARE] = {};
         for (uint32_t at = lane * 8; at < M.hidden; at += 256) {
             float r[8];
             row_values8(router + (int64_t)e * M.ldr, at, M.hidden, M.r_vec, r);
 #pragma unroll
-            for (uint32_t t = 0; t < GROUP; ++t) {
+            for (uint32_t t = 0; t < SHARE; ++t) {
                 if (t0 + t < M.tokens) {
                     float v[8], s = 0.0f;
                     row_values8(x + (int64_t)(t0 + t) * M.ldx, at, M.hidden, M.x_vec, v);
@@ -279,7 +264,7 @@ SQNN_DEV void logits_of_cluster(const MoeArgs &M, double *logits)
             }
         }
 #pragma unroll
-        for (uint32_t t = 0; t < GROUP; ++t) {
+        for (uint32_t t = 0; t < SHARE; ++t) {
 #pragma unroll
             for (uint32_t d = 16; d; d >>= 1) sum[t] += __shfl_xor_sync(0xffffffffu, sum[t], d);
             if (t0 + t < M.tokens && lane < CLUSTER) peer_store(peer_addr(smem_addr(logits + (t0 + t) * M.experts + e), lane), sum[t]);
@@ -331,279 +316,484 @@ SQNN_DEV void choose(const MoeArgs &M, const double *logits, Routing &R)
 
 // ---- first kernel: routing, then h = silu(G x) * (U x) for every (token, expert)
 
-template <typename XT, uint32_t NT>
-__global__ void __launch_bounds__(THREADS, 1) k_moe_up(const MoeArgs M)
+// Exponents of the tokens' largest activations; a warp per token.
+template <typename XT>
+SQNN_DEV void exponents(const MoeArgs &M, Routing &R)
 {
-    extern __shared__ __align__(16) uint8_t smem_raw[];
-    Routing &R = *reinterpret_cast<Routing *>(smem_raw);
-    double *const logits = reinterpret_cast<double *>(smem_raw + ROUTING_BYTES); // [tokens][experts]; after the routing:
-    float *const parts = reinterpret_cast<float *>(smem_raw + ROUTING_BYTES);    // [round's parity][warp][its first or second unit][sum][lane]
-    auto part = [&](uint32_t parity, uint32_t w, uint32_t which, uint32_t j) -> float * { return parts + ((((parity * WARPS + w) * 2 + which) * 4 * NT + j) << 5); };
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (uint32_t t = warp; t < M.tokens; t += WARPS) {
+        const XT *row = static_cast<const XT *>(M.x) + (int64_t)t * M.ldx;
+        uint32_t top = 0;
+        for (uint32_t at = lane * 8; at < M.hidden; at += 256) {
+            float v[8];
+            row_values8(row, at, M.hidden, M.x_vec, v);
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) R.exponent[t] = exponent_of(top);
+    }
+}
+
+// A warp's waits: bounded; once one has given up, its block asks for and waits for nothing any more, and stores nothing.
+struct Waits {
+    volatile uint32_t *abort_flag;
+    uint32_t *status;
+    uint64_t limit;
+    SQNN_DEV void wait(uint32_t bar, uint32_t parity) const
+    {
+        mbar_wait_warp(bar, parity, abort_flag, status, limit);  // (returns at once after a wait that gave up)
+        __syncwarp();
+    }
+};
+
+// The units of all entries form one line, cut into equal runs, one per CTA.  A run is gone through in windows, as many whole entries as
+// there is room for their tokens in shared memory, and a window in rounds of up to STREAMS units, whose columns the warps share evenly.
+struct Walk {
+    uint32_t u, c, left;          // unit, step, and steps to go in this round
+    uint32_t round0, round_n;     // the round's units
+    uint32_t window0, window1;    // the window's units
+};
+
+template <typename XT>
+__global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ CUtensorMap weights, const MoeArgs M)
+{
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    constexpr uint32_t PIECES = sizeof(XT) == 2 ? 1 : 2;
+    __shared__ uint64_t bars[STREAMS * UP_DEPTH];
+    __shared__ uint32_t abort_word;
+    // [rings][routing][partial sums][rows of x]; the logits, [tokens][experts], lie where the rings are later
+    const uint32_t skew = (1024u - (smem_addr(smem_raw) & 1023u)) & 1023u;
+    uint8_t *const smem = smem_raw + skew;
+    static_assert(SQNN_MOE_MAX_LOGITS * sizeof(double) <= STREAMS * UP_DEPTH * UP_SLOT, "room for the logits");
+    Routing &R = *reinterpret_cast<Routing *>(smem + STREAMS * UP_DEPTH * UP_SLOT);
+    double *const logits = reinterpret_cast<double *>(smem);
+    float *const parts = reinterpret_cast<float *>(smem + STREAMS * UP_DEPTH * UP_SLOT + ROUTING_BYTES);
+    uint8_t *const x_rows = reinterpret_cast<uint8_t *>(parts) + PARTS_BYTES;
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
-    constexpr bool EXACT16 = sizeof(XT) == 2;
+    const Waits W{&abort_word, M.status, M.wait_limit};
+    if (tid < STREAMS * UP_DEPTH) mbar_init(smem_addr(bars + tid), 1);
+    if (tid == 0) abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     wait_prior_grid();
     launch_dependents();
     cluster_sync();                                              // all CTAs of the cluster run: their shared memory may be written
     logits_of_cluster<XT>(M, logits);
-    cluster_sync();
+    exponents<XT>(M, R);
+    cluster_sync();                                              // (the last time that one CTA writes to another)
     choose(M, logits, R);
+    fence_async_smem();                                          // the rings' copies come after what was read and written here
     __syncthreads();
-    if (blockIdx.x == 0)
+    list_entries(R, M, M.per);
+    if (blockIdx.x == 0) {                                       // for the caller and for the second kernel
         for (uint32_t i = tid; i < M.tokens * M.top_k; i += THREADS) {
-            M.ids[i] = R.ids[i];
-            M.probs[i] = R.probs[i];
             if (M.ids_out) M.ids_out[i] = R.ids[i];
             if (M.probs_out) M.probs_out[i] = R.probs[i];
         }
-    list_entries(R, M, 8 * NT);
+        for (uint32_t i = tid; i < R.entries * GROUP; i += THREADS) {
+            const uint32_t n = i / GROUP, k = i % GROUP, en = R.entry[n], e = en & 0xffffu, first = (en >> 16) * M.per, count = min(M.per, tokens_of(R, e) - first);
+            Entry &E = M.list[n];
+            if (k == 0) { E.expert = e; E.count = count; }
+            if (k < count) {
+                const uint32_t t = token_of(R, e, first + k), pair = pair_of(R, M, t, e);
+                E.token[k] = t;
+                E.pair[k] = pair;
+                E.prob[k] = R.probs[pair];
+            }
+        }
+        if (tid == 0) *M.list_size = R.entries;
+    }
 
-    const uint32_t groups = (M.inner + 7) / 8, units = R.entries * groups, chunks = (M.hidden + CHUNK - 1) / CHUNK;
+    const uint32_t per_entry = (M.inner + 15) / 16, units = R.entries * per_entry, steps = (M.hidden + STEP - 1) / STEP;
     const uint32_t u0 = (uint32_t)((uint64_t)units * blockIdx.x / gridDim.x), u1 = (uint32_t)((uint64_t)units * (blockIdx.x + 1) / gridDim.x);
-    const uint32_t iblocks = (M.inner + FP8_BLOCK - 1) / FP8_BLOCK, hblocks = (M.hidden + FP8_BLOCK - 1) / FP8_BLOCK;
-    const XT *const x = static_cast<const XT *>(M.x);
-
-    // A warp's way through the rounds: chunk `c` of unit `u`, `left` chunks to go in this round.
-    struct Walk { uint32_t round0, u, c, left; };
-    auto enter = [&](Walk &w, uint32_t round0) {                 // the warp's share of the round that begins at unit round0
+    const uint32_t iblocks = (M.inner + FP8_BLOCK - 1) / FP8_BLOCK;
+    auto tokens_in = [&](uint32_t n) {                           // of entry n
+        const uint32_t en = R.entry[n];
+        return min(M.per, tokens_of(R, en & 0xffffu) - (en >> 16) * M.per);
+    };
+    auto enter = [&](Walk &w, uint32_t round0) {
         w.round0 = round0;
         w.left = 0;
         if (round0 >= u1) return;
-        const uint32_t total = min(WARPS, u1 - round0) * chunks, a = total * warp / WARPS, b = total * (warp + 1) / WARPS;
-        w.u = round0 + a / chunks;
-        w.c = a % chunks;
+        if (round0 >= w.window1) {
+            uint32_t n = round0 / per_entry, rows = 0;
+            while (n < R.entries && n * per_entry < u1 && rows + tokens_in(n) <= M.x_rows) rows += tokens_in(n++);
+            w.window0 = round0;
+            w.window1 = min(u1, n * per_entry);
+        }
+        w.round_n = min(STREAMS, w.window1 - round0);
+        if (warp >= STREAMS) return;
+        const uint32_t total = w.round_n * steps, a = total * warp / STREAMS, b = total * (warp + 1) / STREAMS, d = a / steps;
+        w.u = round0 + d;
+        w.c = a - d * steps;
         w.left = b - a;
     };
-    auto next = [&](Walk &w) {                                   // -> false at the end of the round
-        if (++w.c == chunks) { w.c = 0; ++w.u; }
-        return --w.left != 0;
-    };
-    struct Ring { uint4 gate, up; float sg, su; };
-    Ring ring[AHEAD];
-    Walk ahead;
-    auto request = [&](Ring &r) {                                // the weights of the chunk `ahead` stands at
-        if (ahead.round0 >= u1) return;
-        const uint32_t n = ahead.u / groups, e = R.entry[n] & 0xffffu, row8 = (ahead.u - n * groups) * 8, row = min(row8 + g, M.inner - 1);
-        const uint8_t *p = M.gate_up + (int64_t)e * M.gu_expert + (int64_t)row * M.gu_row;
-        const uint32_t at = ahead.c * CHUNK + t4 * 16;
-        r.gate = row16(p, at, M.hidden);
-        r.up = row16(p + M.gu_half, at, M.hidden);
-        const float *s = M.gate_up_scale + ((uint64_t)(2 * e) * iblocks + row8 / FP8_BLOCK) * hblocks + ahead.c / (FP8_BLOCK / CHUNK);
-        r.sg = __ldg(s);
-        r.su = __ldg(s + (uint64_t)iblocks * hblocks);
-        if (!next(ahead))
-            do enter(ahead, ahead.round0 + WARPS);
-            while (ahead.left == 0 && ahead.round0 < u1);
-    };
-    enter(ahead, u0);
-    while (ahead.left == 0 && ahead.round0 < u1) enter(ahead, ahead.round0 + WARPS);
-#pragma unroll
-    for (uint32_t j = 0; j < AHEAD; ++j) request(ring[j]);
 
-    uint32_t slot = 0, parity = 0;
-    for (uint32_t round0 = u0; round0 < u1; round0 += WARPS, parity ^= 1) {
-        Walk w;
+    // ---- the weights of the step `ahead` stands at, into the ring
+    const uint32_t ring = smem_addr(smem) + warp * UP_DEPTH * UP_SLOT, my_bars = smem_addr(bars) + 8 * warp * UP_DEPTH;
+    Walk ahead;
+    ahead.window1 = ahead.round_n = 0;
+    uint32_t weight_row = 0, put_slot = 0, issued = 0;
+    auto open_unit = [&]() {
+        const uint32_t n = ahead.u / per_entry;
+        weight_row = (R.entry[n] & 0xffffu) * M.gu_expert + (ahead.u - n * per_entry) * 16;
+    };
+    auto request = [&]() {
+        if (ahead.round0 < u1) {
+            if (lane == 0 && !M.skip_loads && !*W.abort_flag) {
+                const uint32_t bar = my_bars + 8 * put_slot, sa = ring + put_slot * UP_SLOT;
+                mbar_expect_tx(bar, UP_SLOT);
+                tma_load_2d(sa, &weights, bar, (int32_t)(ahead.c * STEP), (int32_t)weight_row);
+                tma_load_2d(sa + UP_SLOT / 2, &weights, bar, (int32_t)(ahead.c * STEP), (int32_t)(weight_row + M.gu_half));
+                ++issued;
+            }
+            bool same = true;
+            if (++ahead.c == steps) { ahead.c = 0; ++ahead.u; same = false; }
+            if (--ahead.left == 0) {
+                do enter(ahead, ahead.round0 + ahead.round_n);
+                while (ahead.left == 0 && ahead.round0 < u1);
+                same = false;
+            }
+            if (!same && ahead.round0 < u1) open_unit();
+            put_slot = put_slot + 1 == UP_DEPTH ? 0 : put_slot + 1;
+        }
+    };
+    if (warp < STREAMS) {
+        enter(ahead, u0);
+        while (ahead.left == 0 && ahead.round0 < u1) enter(ahead, ahead.round0 + ahead.round_n);
+        if (ahead.round0 < u1) open_unit();
+#pragma unroll 1
+        for (uint32_t j = 0; j + 1 < UP_DEPTH; ++j) request();
+    }
+
+    Walk w;
+    w.window1 = w.round_n = 0;
+    uint32_t get_slot = 0, get_parity = 0;
+    const uint32_t row_at = matrix_row(lane), lo_at = steps * STEP * 2;
+    const float *unit_scale = nullptr;                           // the unit's scales of G; those of U `to_up` further on
+    const uint64_t to_up = (uint64_t)iblocks * steps;
+    float next_sg = 0.0f, next_su = 0.0f;                        // asked for a step before they are needed
+    auto ask_scales = [&]() {
+        next_sg = __ldg(unit_scale + w.c);
+        next_su = __ldg(unit_scale + to_up + w.c);
+    };
+    auto scales_of_unit = [&]() {
+        const uint32_t n = w.u / per_entry, e = R.entry[n] & 0xffffu, q = w.u - n * per_entry;
+        unit_scale = M.gate_up_scale + ((uint64_t)(2 * e) * iblocks + q / (FP8_BLOCK / 16)) * steps;
+        ask_scales();
+    };
+#pragma unroll 1
+    for (uint32_t round0 = u0; round0 < u1; round0 += w.round_n) {
+        const bool fresh = round0 >= w.window1;
         enter(w, round0);
-        const uint32_t first_unit = w.u;
-        float acc[NT][4];
+        if (w.left) scales_of_unit();
+        if (fresh) {                                             // the window's tokens, scaled and in fp16
+            const uint32_t n0 = w.window0 / per_entry, n1 = (w.window1 + per_entry - 1) / per_entry, cols8 = steps * (STEP / 8);
+            uint32_t base = 0;
+            for (uint32_t n = n0; n < n1; ++n) {
+                const uint32_t en = R.entry[n], e = en & 0xffffu, count = tokens_in(n);
+                for (uint32_t i = tid; i < count * cols8; i += THREADS) {
+                    const uint32_t k = i / cols8, at = (i - k * cols8) * 8, t = token_of(R, e, (en >> 16) * M.per + k);
+                    const float s = scale_of(R.exponent[t]);
+                    float v[8];
+                    row_values8(static_cast<const XT *>(M.x) + (int64_t)t * M.ldx, at, M.hidden, M.x_vec, v);
+                    uint32_t hi[4], lo[4];
 #pragma unroll
-        for (uint32_t k = 0; k < NT; ++k) acc[k][0] = acc[k][1] = acc[k][2] = acc[k][3] = 0.0f;
-        auto put = [&](uint32_t which) {
+                    for (uint32_t j = 0; j < 4; ++j) {
+                        const float a = v[2 * j] * s, b = v[2 * j + 1] * s;
+                        hi[j] = f16x2(a, b);
+                        lo[j] = f16x2(a - f16_lo(hi[j]), b - f16_hi(hi[j]));
+                    }
+                    // columns 16 j + 4 t and on, t even: four at position 16 t + 4 j, the next four at 16 (t + 1) + 4 j
+                    uint8_t *const p = x_rows + (base + k) * M.x_row + (at & ~63u) * 2 + (at & 12u) * 8 + (at >> 4 & 3u) * 8;
+                    *reinterpret_cast<uint2 *>(p) = make_uint2(hi[0], hi[1]);
+                    *reinterpret_cast<uint2 *>(p + 32) = make_uint2(hi[2], hi[3]);
+                    if constexpr (PIECES == 2) {
+                        *reinterpret_cast<uint2 *>(p + lo_at) = make_uint2(lo[0], lo[1]);
+                        *reinterpret_cast<uint2 *>(p + lo_at + 32) = make_uint2(lo[2], lo[3]);
+                    }
+                }
+                base += count;
+            }
+            __syncthreads();
+        }
+        // ---- this warp's steps of the round
+        if (warp < STREAMS) {
+            const uint32_t first_unit = w.u;
+            float acc[8] = {};
+            uint32_t x_at = 0;
+            float b0 = 0.0f, b1 = 0.0f;
+            auto begin = [&]() {                                 // where the tokens of the unit's entry are, and their scales
+                const uint32_t n0 = w.window0 / per_entry, n = w.u / per_entry, en = R.entry[n], e = en & 0xffffu, first = (en >> 16) * M.per, count = tokens_in(n);
+                uint32_t base = 0;
+                for (uint32_t k = n0; k < n; ++k) base += tokens_in(k);
+                x_at = smem_addr(x_rows) + (base + min(g, count - 1)) * M.x_row + t4 * 32;   // columns without a token repeat the last one; nobody looks at them
+                b0 = back_of(R.exponent[token_of(R, e, first + min(2 * t4, count - 1))]);
+                b1 = back_of(R.exponent[token_of(R, e, first + min(2 * t4 + 1, count - 1))]);
+            };
+            if (w.left) begin();
+#pragma unroll 1
+            while (w.left) {
+                W.wait(my_bars + 8 * get_slot, get_parity);
+                const uint32_t sa = ring + get_slot * UP_SLOT + row_at, xa = x_at + w.c * (STEP * 2);
+                const float sg = next_sg, su = next_su;
+                bool end = --w.left == 0;
+                const uint32_t unit = w.u;
+                if (++w.c == steps) { w.c = 0; ++w.u; end = true; }
+                if (!end) ask_scales();
+                else if (w.left) scales_of_unit();
+                float cg[2][4] = {}, cu[2][4] = {};
 #pragma unroll
-            for (uint32_t k = 0; k < NT; ++k)
+                for (uint32_t p = 0; p < 4; ++p) {               // 32 columns
+                    const uint4 hi = shared16(xa + (p >> 1) * 128 + (p & 1) * 16);
+                    uint4 lo;
+                    if constexpr (PIECES == 2) lo = shared16(xa + lo_at + (p >> 1) * 128 + (p & 1) * 16);
+                    const uint4 wg = matrices((sa) ^ (p << 5)), wu = matrices((sa + UP_SLOT / 2) ^ (p << 5));
+                    uint32_t a[4];
+                    weights_of(a, wg.x, wg.y);
+                    mma_f16(cg[p & 1], a, hi.x, hi.y);
+                    if constexpr (PIECES == 2) mma_f16(cg[p & 1], a, lo.x, lo.y);
+                    weights_of(a, wu.x, wu.y);
+                    mma_f16(cu[p & 1], a, hi.x, hi.y);
+                    if constexpr (PIECES == 2) mma_f16(cu[p & 1], a, lo.x, lo.y);
+                    weights_of(a, wg.z, wg.w);
+                    mma_f16(cg[p & 1], a, hi.z, hi.w);
+                    if constexpr (PIECES == 2) mma_f16(cg[p & 1], a, lo.z, lo.w);
+                    weights_of(a, wu.z, wu.w);
+                    mma_f16(cu[p & 1], a, hi.z, hi.w);
+                    if constexpr (PIECES == 2) mma_f16(cu[p & 1], a, lo.z, lo.w);
+                }
+                __syncwarp();                                    // the slot has been read
+                // (asked for three steps ahead: with a ring of four, into the slot before this one, free since the last step)
+                request();
+                if (++get_slot == UP_DEPTH) { get_slot = 0; get_parity ^= 1; }
 #pragma unroll
                 for (uint32_t j = 0; j < 4; ++j) {
-                    part(parity, warp, which, 4 * k + j)[lane] = acc[k][j];
-                    acc[k][j] = 0.0f;
+                    acc[j] = fmaf(cg[0][j] + cg[1][j], sg * (j & 1 ? b1 : b0), acc[j]);
+                    acc[4 + j] = fmaf(cu[0][j] + cu[1][j], su * (j & 1 ? b1 : b0), acc[4 + j]);
                 }
-        };
-        const XT *rows[NT];
-        bool have[NT];
-        auto tokens_of = [&](uint32_t unit) {
-            const uint32_t en = R.entry[unit / groups], e = en & 0xffffu, g0 = (en >> 16) * 8 * NT;
+                if (end) {
+                    float *const p = parts + ((warp * 2 + (unit - first_unit)) * 8) * 32 + lane;
 #pragma unroll
-            for (uint32_t k = 0; k < NT; ++k) {
-                const uint32_t t = token_of(R, e, g0 + 8 * k + g);
-                have[k] = t < MAX_TOKENS;
-                rows[k] = x + (int64_t)(have[k] ? t : 0) * M.ldx;
-            }
-        };
-        if (w.left) tokens_of(w.u);
-        bool more = w.left != 0;
-        while (more) {
-#pragma unroll
-            for (uint32_t j = 0; j < AHEAD; ++j) {
-                if (!more || slot != j) continue;                // (uniform; a round may end anywhere in the ring)
-                float sg, su;
-                uint4 gate, up;
-                gate = ring[j].gate; up = ring[j].up; sg = ring[j].sg; su = ring[j].su;
-                request(ring[j]);
-#pragma unroll
-                for (uint32_t k = 0; k < NT; ++k) {
-                    float v[16];
-                    if (have[k]) values16(rows[k], w.c * CHUNK + t4 * 16, M.hidden, M.x_vec, v);
-                    else
-#pragma unroll
-                        for (uint32_t i = 0; i < 16; ++i) v[i] = 0.0f;
-                    Columns<EXACT16> B;
-                    B.make(v);
-                    float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    multiply(c, gate, up, B);
-                    const float b0 = __shfl_sync(0xffffffffu, B.back, 8 * t4), b1 = __shfl_sync(0xffffffffu, B.back, 8 * t4 + 4);
-                    acc[k][0] = fmaf(c[0], sg * b0, acc[k][0]);
-                    acc[k][1] = fmaf(c[1], sg * b1, acc[k][1]);
-                    acc[k][2] = fmaf(c[2], su * b0, acc[k][2]);
-                    acc[k][3] = fmaf(c[3], su * b1, acc[k][3]);
+                    for (uint32_t j = 0; j < 8; ++j) { p[j * 32] = acc[j]; acc[j] = 0.0f; }
+                    if (w.left) begin();
                 }
-                const uint32_t unit = w.u;
-                more = next(w);
-                slot = slot + 1 == AHEAD ? 0 : slot + 1;
-                if (!more || w.u != unit) put(unit - first_unit);
-                if (more && w.u != unit) tokens_of(w.u);
             }
         }
         __syncthreads();
-        // a warp per unit: its parts in warp order, the gate, and out to h
-        if (warp < min(WARPS, u1 - round0)) {
-            const uint32_t unit = round0 + warp, count = min(WARPS, u1 - round0), total = count * chunks;
-            float sum[NT][4];
+        // ---- a warp per unit: its parts in warp order, the gate, and out to h
+        if (warp < w.round_n && !*W.abort_flag) {
+            const uint32_t unit = round0 + warp, total = w.round_n * steps;
+            float sum[8] = {};
+            for (uint32_t q = 0; q < STREAMS; ++q) {
+                const uint32_t a = total * q / STREAMS, b = total * (q + 1) / STREAMS;
+                if (a >= b || b <= warp * steps || a >= (warp + 1) * steps) continue;
+                const float *const p = parts + ((q * 2 + (warp - a / steps)) * 8) * 32 + lane;
 #pragma unroll
-            for (uint32_t k = 0; k < NT; ++k) sum[k][0] = sum[k][1] = sum[k][2] = sum[k][3] = 0.0f;
-            for (uint32_t q = 0; q < WARPS; ++q) {
-                const uint32_t a = total * q / WARPS, b = total * (q + 1) / WARPS;
-                if (a >= b || b <= warp * chunks || a >= (warp + 1) * chunks) continue;
-                const uint32_t which = warp - a / chunks;
-#pragma unroll
-                for (uint32_t k = 0; k < NT; ++k)
-#pragma unroll
-                    for (uint32_t j = 0; j < 4; ++j) sum[k][j] += part(parity, q, which, 4 * k + j)[lane];
+                for (uint32_t j = 0; j < 8; ++j) sum[j] += p[j * 32];
             }
-            const uint32_t en = R.entry[unit / groups], e = en & 0xffffu, g0 = (en >> 16) * 8 * NT, row = unit % groups * 8 + g;
+            const uint32_t n = unit / per_entry, en = R.entry[n], e = en & 0xffffu, q = unit - n * per_entry, count = tokens_in(n);
+            const uint32_t i = q * 16 + g;                       // rows i and i + 8
+            // where a row's value goes: 16 (row / 4 % 4) + 4 (q % 4) + row % 4 of its 64
+            const uint32_t at = q / (STEP / 16) * H_BLOCK + ((q & 4) * 16 + (g >> 2) * 16 + (q & 3) * 4 + (g & 3)) * 2;
 #pragma unroll
-            for (uint32_t k = 0; k < NT; ++k)
+            for (uint32_t k = 0; k < 2; ++k) {
+                const float a = sum[k], b = sum[2 + k];
+                const float va = i < M.inner ? a / (1.0f + expf(-a)) * sum[4 + k] : 0.0f;
+                const float vb = i + 8 < M.inner ? b / (1.0f + expf(-b)) * sum[6 + k] : 0.0f;
+                uint32_t top = max(__float_as_uint(va) & 0x7fffffffu, __float_as_uint(vb) & 0x7fffffffu);
 #pragma unroll
-                for (uint32_t j = 0; j < 2; ++j) {
-                    const uint32_t t = token_of(R, e, g0 + 8 * k + 2 * t4 + j);
-                    if (t < MAX_TOKENS && row < M.inner) {
-                        const float a = sum[k][j];
-                        M.h[(uint64_t)pair_of(R, M, t, e) * M.pitch + row] = a / (1.0f + expf(-a)) * sum[k][2 + j];
-                    }
+                for (uint32_t d = 4; d < 32; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+                const uint32_t ex = exponent_of(top);
+                const float s = scale_of(ex);
+                const uint32_t hi = f16x2(va * s, vb * s), lo = f16x2(va * s - f16_lo(hi), vb * s - f16_hi(hi));
+                const uint32_t column = 2 * t4 + k;
+                if (column < count) {
+                    const uint32_t t = token_of(R, e, (en >> 16) * M.per + column);
+                    uint8_t *const row = M.h + (uint64_t)pair_of(R, M, t, e) * M.h_row;
+                    *reinterpret_cast<uint16_t *>(row + at) = (uint16_t)hi;
+                    *reinterpret_cast<uint16_t *>(row + at + 64) = (uint16_t)(hi >> 16);
+                    *reinterpret_cast<uint16_t *>(row + at + 256) = (uint16_t)lo;
+                    *reinterpret_cast<uint16_t *>(row + at + 320) = (uint16_t)(lo >> 16);
+                    if (g == 0) *reinterpret_cast<float *>(row + q / 8 * H_BLOCK + 512 + (q & 7) * 4) = back_of(ex);
+                    if (q + 1 == per_entry)                      // the rest of the last block is zero
+                        for (uint32_t z = q + 1; z & 7; ++z) {
+                            const uint32_t to = z / 8 * H_BLOCK + ((z & 4) * 16 + (g >> 2) * 16 + (z & 3) * 4 + (g & 3)) * 2;
+                            *reinterpret_cast<uint16_t *>(row + to) = *reinterpret_cast<uint16_t *>(row + to + 64) = 0;
+                            *reinterpret_cast<uint16_t *>(row + to + 256) = *reinterpret_cast<uint16_t *>(row + to + 320) = 0;
+                            if (g == 0) *reinterpret_cast<float *>(row + z / 8 * H_BLOCK + 512 + (z & 7) * 4) = 0.0f;
+                        }
                 }
+            }
         }
+        __syncthreads();
     }
-    // no CTA leaves while another one of its cluster may still write to it: all such writes were before the second cluster_sync
+    // after a wait that gave up: copies in flight must land before the block's shared memory goes away
+    if (warp < STREAMS && lane == 0 && *W.abort_flag)
+        for (uint32_t s = 0; s < UP_DEPTH; ++s) {
+            const uint32_t uses = (issued + UP_DEPTH - 1 - s) / UP_DEPTH;
+            if (uses) mbar_drain(my_bars + 8 * s, (uses - 1) & 1u, M.wait_limit);
+        }
 }
 
 // ---- second kernel: y = sum p D h
 
-template <uint32_t NT>
-__global__ void __launch_bounds__(THREADS, 1) k_moe_down(const MoeArgs M)
+template <uint32_t ROWS>
+__global__ void __launch_bounds__(STREAMS * 32, 1) k_moe_down(const __grid_constant__ CUtensorMap weights, const MoeArgs M)
 {
-    extern __shared__ __align__(16) uint8_t smem_raw[];
-    Routing &R = *reinterpret_cast<Routing *>(smem_raw);
-    float *const sums = reinterpret_cast<float *>(smem_raw + ROUTING_BYTES);     // [warp][token][16 rows]
-    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
-    const uint32_t row0 = blockIdx.x * 16;
-    float *const mine = sums + (uint64_t)warp * M.tokens * 16;
-    for (uint32_t i = lane; i < M.tokens * 16; i += 32) mine[i] = 0.0f;
+    constexpr uint32_t TILES = ROWS / 16, W_BYTES = ROWS * STEP;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ uint64_t bars[STREAMS * MAX_DOWN_DEPTH];
+    __shared__ uint32_t abort_word;
+    // [ring of weights][ring of inner values][sums: warp, token, row]
+    const uint32_t skew = (1024u - (smem_addr(smem_raw) & 1023u)) & 1023u, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+    uint8_t *const smem = smem_raw + skew;
+    const uint32_t h_slot = M.slot - W_BYTES, ring = smem_addr(smem) + warp * M.depth * W_BYTES;
+    const uint32_t h_ring = smem_addr(smem) + STREAMS * M.depth * W_BYTES + warp * M.depth * h_slot, my_bars = smem_addr(bars) + 8 * warp * MAX_DOWN_DEPTH;
+    float *const sums = reinterpret_cast<float *>(smem + (size_t)STREAMS * M.depth * M.slot);
+    float *const mine = sums + warp * M.tokens * ROWS;
+    const uint32_t row0 = blockIdx.x * ROWS;
+    const Waits W{&abort_word, M.status, M.wait_limit};
+    for (uint32_t i = lane; i < M.tokens * ROWS; i += 32) mine[i] = 0.0f;
+    if (lane < M.depth) mbar_init(my_bars + 8 * lane, 1);
+    if (tid == 0) abort_word = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    __syncthreads();
     wait_prior_grid();
     launch_dependents();
-    for (uint32_t i = tid; i < M.tokens * M.top_k; i += THREADS) {
-        R.ids[i] = M.ids[i];
-        R.probs[i] = M.probs[i];
-    }
-    __syncthreads();
-    list_entries(R, M, 8 * NT);
-    const uint32_t chunks = (M.inner + CHUNK - 1) / CHUNK, total = R.entries * chunks;
-    const uint32_t q0 = (uint32_t)((uint64_t)total * warp / WARPS), q1 = (uint32_t)((uint64_t)total * (warp + 1) / WARPS);
-    const uint32_t iblocks = (M.inner + FP8_BLOCK - 1) / FP8_BLOCK, hblocks = (M.hidden + FP8_BLOCK - 1) / FP8_BLOCK;
-    const uint32_t ra = min(row0 + g, M.hidden - 1), rb = min(row0 + g + 8, M.hidden - 1);
+    asm volatile("fence.proxy.async.global;\n" ::: "memory");    // the copies below read what the first kernel stored
+    const uint32_t steps = (M.inner + STEP - 1) / STEP, total = *M.list_size * steps;
+    const uint32_t q0 = (uint32_t)((uint64_t)total * warp / STREAMS), q1 = (uint32_t)((uint64_t)total * (warp + 1) / STREAMS);
 
-    struct Ring { uint4 a, b; float s; };
-    Ring ring[AHEAD];
-    uint32_t ahead_n = q0 / chunks, ahead_c = q0 % chunks, ahead_q = q0;
-    auto request = [&](Ring &r) {
-        if (ahead_q >= q1) return;
-        const uint32_t e = R.entry[ahead_n] & 0xffffu;
-        const uint8_t *p = M.down + (int64_t)e * M.d_expert;
-        const uint32_t at = ahead_c * CHUNK + t4 * 16;
-        r.a = row16(p + (int64_t)ra * M.d_row, at, M.inner);
-        r.b = row16(p + (int64_t)rb * M.d_row, at, M.inner);
-        r.s = __ldg(M.down_scale + ((uint64_t)e * hblocks + row0 / FP8_BLOCK) * iblocks + ahead_c / (FP8_BLOCK / CHUNK));
-        ++ahead_q;
-        if (++ahead_c == chunks) { ahead_c = 0; ++ahead_n; }
+    // ---- a step's weights and its tokens' inner values into the rings
+    uint32_t ahead_n = q0 / steps, ahead_c = q0 - ahead_n * steps, ahead_q = q0, put_slot = 0, issued = 0;
+    uint32_t weight_row = 0, ahead_count = 0;
+    const uint8_t *h_row = nullptr;                              // of token `lane`
+    auto open_entry = [&]() {
+        const Entry &E = M.list[ahead_n];
+        ahead_count = E.count;
+        weight_row = E.expert * M.d_expert + row0;
+        h_row = M.h + (uint64_t)E.pair[lane < ahead_count ? lane : 0] * M.h_row;
     };
-#pragma unroll
-    for (uint32_t j = 0; j < AHEAD; ++j) request(ring[j]);
-
-    uint32_t n = q0 / chunks, c_at = q0 % chunks;
-    float acc[NT][4];
-    const float *rows[NT];
-    bool have[NT];
-    auto begin = [&]() {
-        const uint32_t en = R.entry[n], e = en & 0xffffu, g0 = (en >> 16) * 8 * NT;
-#pragma unroll
-        for (uint32_t k = 0; k < NT; ++k) {
-            acc[k][0] = acc[k][1] = acc[k][2] = acc[k][3] = 0.0f;
-            const uint32_t t = token_of(R, e, g0 + 8 * k + g);
-            have[k] = t < MAX_TOKENS;
-            rows[k] = M.h + (have[k] ? (uint64_t)pair_of(R, M, t, e) * M.pitch : 0);
+    auto request = [&]() {
+        if (ahead_q < q1) {
+            const uint32_t bar = my_bars + 8 * put_slot;
+            const bool go = !M.skip_loads && !*W.abort_flag;
+            if (lane == 0 && go) {
+                mbar_expect_tx(bar, W_BYTES + ahead_count * H_BLOCK);
+                tma_load_2d(ring + put_slot * W_BYTES, &weights, bar, (int32_t)(ahead_c * STEP), (int32_t)weight_row);
+                ++issued;
+            }
+            const bool all_go = __shfl_sync(0xffffffffu, (int)go, 0) != 0;
+            if (lane < ahead_count && all_go) bulk_load(h_ring + put_slot * h_slot + lane * H_PITCH, h_row + (uint64_t)ahead_c * H_BLOCK, H_BLOCK, bar);
+            ++ahead_q;
+            if (++ahead_c == steps) {
+                ahead_c = 0;
+                ++ahead_n;
+                if (ahead_q < q1) open_entry();
+            }
+            put_slot = put_slot + 1 == M.depth ? 0 : put_slot + 1;
         }
     };
-    auto end = [&]() {                                           // an expert's part goes to the warp's sums
-        const uint32_t en = R.entry[n], e = en & 0xffffu, g0 = (en >> 16) * 8 * NT;
+    if (q0 < q1) open_entry();
+#pragma unroll 1
+    for (uint32_t j = 0; j + 1 < M.depth; ++j) request();
+
+    uint32_t n = q0 / steps, c_at = q0 - n * steps, get_slot = 0, get_parity = 0, count = 0;
+    const uint32_t row_at = matrix_row(lane);
+    float acc[TILES][4] = {};
+    // of the entry at hand and of the next one; D's scale is asked for a step before it is needed
+    uint32_t next_expert = 0, next_count = 0;
+    const float *entry_scale = nullptr;
+    float next_s = 0.0f;
+    auto scales_of = [&](uint32_t expert) { return M.down_scale + ((uint64_t)expert * ((M.hidden + FP8_BLOCK - 1) / FP8_BLOCK) + row0 / FP8_BLOCK) * steps; };
+    auto look_ahead = [&]() {
+        if ((uint64_t)(n + 1) * steps < q1) {
+            next_expert = M.list[n + 1].expert;
+            next_count = M.list[n + 1].count;
+        }
+    };
+    if (q0 < q1) {
+        count = M.list[n].count;
+        entry_scale = scales_of(M.list[n].expert);
+        next_s = __ldg(entry_scale + c_at);
+        look_ahead();
+    }
+#pragma unroll 1
+    for (uint32_t q = q0; q < q1; ++q) {
+        W.wait(my_bars + 8 * get_slot, get_parity);
+        const uint32_t sa = ring + get_slot * W_BYTES + row_at, b = h_ring + get_slot * h_slot + min(g, count - 1) * H_PITCH + t4 * 32;
+        const uint32_t f_at = h_ring + get_slot * h_slot + 512, f0_at = f_at + min(2 * t4, count - 1) * H_PITCH, f1_at = f_at + min(2 * t4 + 1, count - 1) * H_PITCH;
+        const float s = next_s;
+        if (c_at + 1 < steps) next_s = __ldg(entry_scale + c_at + 1);
+        else if (q + 1 < q1) next_s = __ldg(entry_scale = scales_of(next_expert));
+        float part[TILES][4] = {};                               // of this step, before D's scale
 #pragma unroll
-        for (uint32_t k = 0; k < NT; ++k)
+        for (uint32_t p = 0; p < 4; ++p) {                       // 32 columns
+            const uint4 hi = shared16(b + (p >> 1) * 128 + (p & 1) * 16), lo = shared16(b + 256 + (p >> 1) * 128 + (p & 1) * 16);
+            const float f0[2] = {shared4(f0_at + p * 8), shared4(f0_at + p * 8 + 4)}, f1[2] = {shared4(f1_at + p * 8), shared4(f1_at + p * 8 + 4)};
 #pragma unroll
-            for (uint32_t j = 0; j < 2; ++j) {
-                const uint32_t t = token_of(R, e, g0 + 8 * k + 2 * t4 + j);
-                if (t < MAX_TOKENS) {
-                    const float p = R.probs[pair_of(R, M, t, e)];
-                    float *const s = mine + t * 16 + g;
-                    s[0] = fmaf(p, acc[k][j], s[0]);
-                    s[8] = fmaf(p, acc[k][2 + j], s[8]);
+            for (uint32_t r = 0; r < TILES; ++r) {
+                const uint4 w = matrices((sa + r * (16 * STEP)) ^ (p << 5));
+#pragma unroll
+                for (uint32_t j = 0; j < 2; ++j) {
+                    uint32_t a[4];
+                    weights_of(a, j ? w.z : w.x, j ? w.w : w.y);
+                    float c[4] = {};
+                    mma_f16(c, a, j ? hi.z : hi.x, j ? hi.w : hi.y);
+                    mma_f16(c, a, j ? lo.z : lo.x, j ? lo.w : lo.y);
+                    part[r][0] = fmaf(c[0], f0[j], part[r][0]);
+                    part[r][1] = fmaf(c[1], f1[j], part[r][1]);
+                    part[r][2] = fmaf(c[2], f0[j], part[r][2]);
+                    part[r][3] = fmaf(c[3], f1[j], part[r][3]);
                 }
             }
-        __syncwarp();
-    };
-    if (q0 < q1) begin();
-    for (uint32_t q = q0; q < q1;) {
+        }
+        __syncwarp();                                            // the slot has been read
+        request();
+        if (++get_slot == M.depth) { get_slot = 0; get_parity ^= 1; }
 #pragma unroll
-        for (uint32_t j = 0; j < AHEAD; ++j) {
-            if (q >= q1) break;
-            const uint4 a = ring[j].a, b = ring[j].b;
-            const float s = ring[j].s;
-            request(ring[j]);
+        for (uint32_t r = 0; r < TILES; ++r)
 #pragma unroll
-            for (uint32_t k = 0; k < NT; ++k) {
-                float v[16];
-                if (have[k]) values16(rows[k], c_at * CHUNK + t4 * 16, M.inner, true, v);
-                else
+            for (uint32_t j = 0; j < 4; ++j) acc[r][j] = fmaf(part[r][j], s, acc[r][j]);
+        if (++c_at == steps || q + 1 == q1) {                    // the entry's part goes to the warp's sums
+            const Entry &E = M.list[n];
 #pragma unroll
-                    for (uint32_t i = 0; i < 16; ++i) v[i] = 0.0f;
-                Columns<false> B;
-                B.make(v);
-                float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                multiply(c, a, b, B);
-                const float b0 = __shfl_sync(0xffffffffu, B.back, 8 * t4) * s, b1 = __shfl_sync(0xffffffffu, B.back, 8 * t4 + 4) * s;
-                acc[k][0] = fmaf(c[0], b0, acc[k][0]);
-                acc[k][1] = fmaf(c[1], b1, acc[k][1]);
-                acc[k][2] = fmaf(c[2], b0, acc[k][2]);
-                acc[k][3] = fmaf(c[3], b1, acc[k][3]);
-            }
-            ++q;
-            if (++c_at == chunks || q == q1) {
-                end();
-                if (c_at == chunks) { c_at = 0; ++n; }
-                if (q < q1) begin();
+            for (uint32_t k = 0; k < 2; ++k)
+                if (2 * t4 + k < count) {
+                    const float p = E.prob[2 * t4 + k];
+                    float *const to = mine + E.token[2 * t4 + k] * ROWS + g;
+#pragma unroll
+                    for (uint32_t r = 0; r < TILES; ++r) {
+                        to[16 * r] = fmaf(p, acc[r][k], to[16 * r]);
+                        to[16 * r + 8] = fmaf(p, acc[r][2 + k], to[16 * r + 8]);
+                    }
+                }
+#pragma unroll
+            for (uint32_t r = 0; r < TILES; ++r) acc[r][0] = acc[r][1] = acc[r][2] = acc[r][3] = 0.0f;
+            __syncwarp();
+            if (c_at == steps) {
+                c_at = 0;
+                ++n;
+                count = next_count;
+                look_ahead();
             }
         }
     }
     __syncthreads();
-    for (uint32_t i = tid; i < M.tokens * 16; i += THREADS) {
-        const uint32_t t = i >> 4, row = row0 + (i & 15);
+    if (*W.abort_flag) {                                         // copies in flight must land before the block's shared memory goes away
+        if (lane == 0)
+            for (uint32_t s = 0; s < M.depth; ++s) {
+                const uint32_t uses = (issued + M.depth - 1 - s) / M.depth;
+                if (uses) mbar_drain(my_bars + 8 * s, (uses - 1) & 1u, M.wait_limit);
+            }
+        return;
+    }
+    for (uint32_t i = tid; i < M.tokens * ROWS; i += STREAMS * 32) {
+        const uint32_t t = i / ROWS, row = row0 + i % ROWS;
         float s = 0.0f;
 #pragma unroll
-        for (uint32_t w = 0; w < WARPS; ++w) s += sums[(uint64_t)w * M.tokens * 16 + i];
+        for (uint32_t w = 0; w < STREAMS; ++w) s += sums[w * M.tokens * ROWS + i];
         if (row < M.hidden) {
             const int64_t at = (int64_t)t * M.ldy + row;
             if (M.y_bf16) static_cast<__nv_bfloat16 *>(M.y)[at] = __float2bfloat16_rn(s);
@@ -614,26 +804,51 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_down(const MoeArgs M)
 
 // ---- host
 
-struct MoeShape { uint32_t pairs, pitch; size_t h_bytes, ids_bytes, bytes; };
+struct MoeShape { uint32_t h_row; size_t h_bytes, bytes; };
 MoeShape moe_shape(uint32_t tokens, uint32_t top_k, uint64_t inner)
 {
     MoeShape s;
-    s.pairs = tokens * top_k;
-    s.pitch = (uint32_t)((inner + 31) / 32 * 32);
-    s.h_bytes = ((size_t)s.pairs * s.pitch * 4 + 255) / 256 * 256;
-    s.ids_bytes = ((size_t)s.pairs * 4 + 255) / 256 * 256;
-    s.bytes = s.h_bytes + 2 * s.ids_bytes;
+    const size_t pairs = (size_t)tokens * top_k;
+    s.h_row = (uint32_t)((inner + STEP - 1) / STEP * H_BLOCK);
+    s.h_bytes = (pairs * s.h_row + 255) / 256 * 256;
+    s.bytes = s.h_bytes + 256 + (pairs * sizeof(Entry) + 255) / 256 * 256;       // an entry has a token at least
     return s;
 }
 
-template <typename XT, uint32_t NT>
-int launch_moe(const MoeArgs &M, cudaStream_t st)
+// Rows of 8-bit weights, boxes of `box_rows` by 128 columns, swizzled.
+bool make_map(CUtensorMap *map, const void *p, uint32_t n, uint64_t rows, int64_t ld, uint32_t box_rows)
 {
-    auto up = k_moe_up<XT, NT>;
-    auto down = k_moe_down<NT>;
-    const size_t logits = (size_t)M.tokens * M.experts * sizeof(double), parts = (size_t)2 * WARPS * 2 * 4 * NT * 32 * sizeof(float);
-    const size_t smem_up = ROUTING_BYTES + (logits > parts ? logits : parts), smem_down = ROUTING_BYTES + (size_t)WARPS * M.tokens * 16 * sizeof(float);
-    if (ensure_dynamic_smem(reinterpret_cast<const void *>(up), smem_up) != SQNN_OK) return SQNN_E_CUDA;
+    EncodeTiledFn encode = encode_tiled_fn();
+    if (!encode) return false;
+    const cuuint64_t gdim[2] = {n, rows}, gstride[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {STEP, box_rows}, estride[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(p), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename XT>
+int launch_moe(MoeArgs M, const sqnn_moe *L, cudaStream_t st)
+{
+    auto up = k_moe_up<XT>;
+    // first kernel: what the ring and the partial sums leave holds rows of x
+    const uint32_t cols = (M.hidden + STEP - 1) / STEP * STEP, pieces = sizeof(XT) == 2 ? 1 : 2;
+    const size_t fixed = 1024 + STREAMS * UP_DEPTH * UP_SLOT + ROUTING_BYTES + PARTS_BYTES;
+    M.x_row = cols * 2 * pieces + 16;                            // 16 bytes past a multiple of 128: neighbouring rows in neighbouring banks
+    M.x_rows = (uint32_t)((SMEM_BYTES - fixed) / M.x_row);
+    if (M.x_rows == 0) return SQNN_E_UNSUPPORTED;
+    M.per = M.x_rows < GROUP ? M.x_rows : GROUP;
+    // second kernel: 32 rows per CTA where that still makes two CTAs for three SMs; as deep a ring as there is room for
+    const uint32_t rows = 3 * ((M.hidden + 31) / 32) >= 2 * (uint32_t)sm_count() ? 32 : 16;
+    M.slot = rows * STEP + (M.tokens < M.per ? M.tokens : M.per) * H_PITCH;
+    const size_t sums = (size_t)STREAMS * M.tokens * rows * 4;
+    M.depth = (uint32_t)((SMEM_BYTES - 1024 - sums) / (STREAMS * M.slot));
+    M.depth = M.depth < MAX_DOWN_DEPTH ? M.depth : MAX_DOWN_DEPTH;
+    const size_t smem_down = 1024 + sums + (size_t)STREAMS * M.depth * M.slot;
+    CUtensorMap gu_map, d_map;
+    if (!make_map(&gu_map, L->gate_up, M.hidden, (uint64_t)(M.experts - 1) * M.gu_expert + M.gu_half + M.inner, L->gate_up_row, 16) ||
+        !make_map(&d_map, L->down, M.inner, (uint64_t)(M.experts - 1) * M.d_expert + M.hidden, L->down_row, rows))
+        return SQNN_E_CUDA;
+    if (ensure_dynamic_smem(reinterpret_cast<const void *>(up), SMEM_BYTES) != SQNN_OK) return SQNN_E_CUDA;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = CLUSTER;
@@ -643,11 +858,11 @@ int launch_moe(const MoeArgs &M, cudaStream_t st)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(CLUSTER);
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = smem_up;
+    cfg.dynamicSmemBytes = SMEM_BYTES;
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    // as many CTAs as run at once in whole clusters, asked for once per device (threads and registers decide, not shared memory: one per SM)
+    // as many CTAs as run at once in whole clusters, asked for once per device
     static std::atomic<int> known[64];
     int dev = 0, clusters = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SQNN_E_CUDA;
@@ -658,12 +873,12 @@ int launch_moe(const MoeArgs &M, cudaStream_t st)
     }
     cfg.gridDim = dim3((uint32_t)clusters * CLUSTER);
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, up, M) != cudaSuccess) return SQNN_E_CUDA;
-    return launch_kernel(down, (M.hidden + 15) / 16, THREADS, smem_down, st, M);
+    if (cudaLaunchKernelEx(&cfg, up, gu_map, M) != cudaSuccess) return SQNN_E_CUDA;
+    return launch_kernel(rows == 32 ? k_moe_down<32> : k_moe_down<16>, (M.hidden + rows - 1) / rows, STREAMS * 32, smem_down, st, d_map, M);
 }
 
 int moe_queue(const sqnn_moe *L, uint32_t tokens, const void *d_x, int x_dtype, int64_t ldx, void *d_y, int y_dtype, int64_t ldy,
-              int32_t *d_ids, float *d_probs, void *d_workspace, size_t workspace_bytes, cudaStream_t st)
+              int32_t *d_ids, float *d_probs, void *d_workspace, size_t workspace_bytes, uint32_t *d_status, cudaStream_t st)
 {
     const auto known_type = [](int t) { return t == SQNN_X_F32 || t == SQNN_X_BF16; };
     const auto aligned_to = [](const void *p, uintptr_t size) { return ((uintptr_t)p & (size - 1)) == 0; };
@@ -672,7 +887,7 @@ int moe_queue(const sqnn_moe *L, uint32_t tokens, const void *d_x, int x_dtype, 
     if (L->experts == 0 || L->top_k == 0 || L->top_k > L->experts || L->hidden == 0 || L->inner == 0) return SQNN_E_INVALID_ARG;
     if (!known_type(x_dtype) || !known_type(y_dtype)) return SQNN_E_INVALID_ARG;
     if (tokens > SQNN_MOE_MAX_TOKENS || L->experts > SQNN_MOE_MAX_EXPERTS || L->top_k > SQNN_MOE_MAX_TOP_K || tokens * L->experts > SQNN_MOE_MAX_LOGITS ||
-        L->hidden > (1u << 20) || L->inner > (1u << 20))
+        L->hidden > SQNN_MOE_MAX_WIDTH || L->inner > SQNN_MOE_MAX_WIDTH)
         return SQNN_E_UNSUPPORTED;
     const int64_t hidden = L->hidden, inner = L->inner;
     const uintptr_t xs = x_dtype == SQNN_X_BF16 ? 2 : 4, ys = y_dtype == SQNN_X_BF16 ? 2 : 4;
@@ -682,29 +897,36 @@ int moe_queue(const sqnn_moe *L, uint32_t tokens, const void *d_x, int x_dtype, 
     if (!aligned_to(d_x, xs) || !aligned_to(L->router, xs) || !aligned_to(d_y, ys) || !aligned_to(L->gate_up_scale, 4) || !aligned_to(L->down_scale, 4) ||
         !aligned_to(d_ids, 4) || !aligned_to(d_probs, 4))
         return SQNN_E_INVALID_ARG;
-    if (!aligned_to(L->gate_up, 16) || !aligned_to(L->down, 16) || ((L->gate_up_row | L->gate_up_half | L->gate_up_expert | L->down_row | L->down_expert) & 15))
+    if (!aligned_to(L->gate_up, 16) || !aligned_to(L->down, 16) || ((L->gate_up_row | L->down_row) & 15)) return SQNN_E_UNSUPPORTED;
+    // the weights of all experts are rows of one matrix to the copies
+    const int64_t most_rows = 1ll << 30;
+    if (L->gate_up_half % L->gate_up_row || L->gate_up_expert % L->gate_up_row || L->down_expert % L->down_row || L->gate_up_row > (1ll << 30) || L->down_row > (1ll << 30) ||
+        L->gate_up_expert / L->gate_up_row * L->experts + L->gate_up_half / L->gate_up_row + inner > most_rows || L->down_expert / L->down_row * L->experts + hidden > most_rows)
         return SQNN_E_UNSUPPORTED;
     const MoeShape shape = moe_shape(tokens, L->top_k, L->inner);
     if (!d_workspace || workspace_bytes < shape.bytes || !aligned_to(d_workspace, 256)) return SQNN_E_WORKSPACE;
     MoeArgs M = {};
-    M.x = d_x; M.router = L->router; M.gate_up = L->gate_up; M.down = L->down;
+    M.x = d_x; M.router = L->router;
     M.gate_up_scale = L->gate_up_scale; M.down_scale = L->down_scale;
     M.y = d_y;
-    M.h = static_cast<float *>(d_workspace);
-    M.ids = reinterpret_cast<int32_t *>(static_cast<uint8_t *>(d_workspace) + shape.h_bytes);
-    M.probs = reinterpret_cast<float *>(static_cast<uint8_t *>(d_workspace) + shape.h_bytes + shape.ids_bytes);
+    M.h = static_cast<uint8_t *>(d_workspace);
+    M.list_size = reinterpret_cast<uint32_t *>(M.h + shape.h_bytes);
+    M.list = reinterpret_cast<Entry *>(M.h + shape.h_bytes + 256);
     M.ids_out = d_ids; M.probs_out = d_probs;
     M.ldx = ldx; M.ldr = L->router_row; M.ldy = ldy;
-    M.gu_expert = L->gate_up_expert; M.gu_half = L->gate_up_half; M.gu_row = L->gate_up_row;
-    M.d_expert = L->down_expert; M.d_row = L->down_row;
-    M.tokens = tokens; M.experts = L->experts; M.top_k = L->top_k; M.hidden = L->hidden; M.inner = L->inner; M.pitch = shape.pitch;
+    M.gu_expert = (uint32_t)(L->gate_up_expert / L->gate_up_row); M.gu_half = (uint32_t)(L->gate_up_half / L->gate_up_row);
+    M.d_expert = (uint32_t)(L->down_expert / L->down_row);
+    M.tokens = tokens; M.experts = L->experts; M.top_k = L->top_k; M.hidden = L->hidden; M.inner = L->inner;
+    M.h_row = shape.h_row;
+    const DebugKnobs dbg = debug_knobs();
+    M.skip_loads = (dbg.flags & 16u) ? 1u : 0u;
+    M.wait_limit = dbg.wait_cycles ? dbg.wait_cycles : WAIT_LIMIT_CYCLES;
+    M.status = d_status;
     M.renormalize = L->renormalize;
     M.x_vec = aligned_to(d_x, 16) && (ldx * (int64_t)xs) % 16 == 0;
     M.r_vec = aligned_to(L->router, 16) && (L->router_row * (int64_t)xs) % 16 == 0;
     M.y_bf16 = y_dtype == SQNN_X_BF16;
-    // up to eight tokens of an expert are multiplied together, from nine tokens on up to sixteen
-    if (x_dtype == SQNN_X_BF16) return tokens <= 8 ? launch_moe<__nv_bfloat16, 1>(M, st) : launch_moe<__nv_bfloat16, 2>(M, st);
-    return tokens <= 8 ? launch_moe<float, 1>(M, st) : launch_moe<float, 2>(M, st);
+    return x_dtype == SQNN_X_BF16 ? launch_moe<__nv_bfloat16>(M, L, st) : launch_moe<float>(M, L, st);
 }
 
 }  // namespace
@@ -717,10 +939,11 @@ extern "C" size_t sqnn_moe_workspace_bytes(uint32_t tokens, uint32_t top_k, uint
 }
 
 extern "C" int sqnn_moe_fp8(const sqnn_moe *layer, uint32_t tokens, const void *d_x, int x_dtype, int64_t ldx, void *d_y, int y_dtype, int64_t ldy,
-                            int32_t *d_ids, float *d_probs, void *d_workspace, size_t workspace_bytes, void *cuda_stream)
+                            int32_t *d_ids, float *d_probs, void *d_workspace, size_t workspace_bytes, uint32_t *d_status,
+                            void *cuda_stream)
 {
     sqnn::ApiScope scope("sqnn_moe_fp8");
     return scope.finish(sqnn::moe_queue(layer, tokens, d_x, x_dtype, ldx, d_y, y_dtype, ldy, d_ids, d_probs, d_workspace, workspace_bytes,
-                                        (cudaStream_t)cuda_stream),
-                        nullptr, (cudaStream_t)cuda_stream);
+                                        d_status, (cudaStream_t)cuda_stream),
+                        d_status, (cudaStream_t)cuda_stream);
 }

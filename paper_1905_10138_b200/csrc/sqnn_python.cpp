@@ -351,14 +351,14 @@ PyObject *fp8_matmul(PyObject *, PyObject *const *a, Py_ssize_t nargs)
     });
 }
 
-// moe_fp8(x, router, top_k, renormalize, gate_up, gate_up_scale, down, down_scale, y, workspace, ids, probs, stream) -> status code
+// moe_fp8(x, router, top_k, renormalize, gate_up, gate_up_scale, down, down_scale, y, workspace, ids, probs, status, stream) -> status code
 PyObject *moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs)
 {
     return guarded([&]() -> PyObject * {
-        if (!enough(nargs, 13)) return nullptr;
-        const at::Tensor *x, *router, *gu, *gus, *down, *downs, *y, *ws, *ids, *probs;
+        if (!enough(nargs, 14)) return nullptr;
+        const at::Tensor *x, *router, *gu, *gus, *down, *downs, *y, *ws, *ids, *probs, *status;
         void *st;
-        if (!tensor_arg(a[0], &x) || !tensor_arg(a[1], &router) || !tensor_arg(a[4], &gu) || !tensor_arg(a[5], &gus) || !tensor_arg(a[6], &down) ||
+        if (!tensor_arg(a[12], &status) || !tensor_arg(a[0], &x) || !tensor_arg(a[1], &router) || !tensor_arg(a[4], &gu) || !tensor_arg(a[5], &gus) || !tensor_arg(a[6], &down) ||
             !tensor_arg(a[7], &downs) || !tensor_arg(a[8], &y) || !tensor_arg(a[9], &ws) || !tensor_arg(a[10], &ids) || !tensor_arg(a[11], &probs))
             return nullptr;
         const long top_k = PyLong_AsLong(a[2]);
@@ -400,10 +400,11 @@ PyObject *moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs)
             fail("probs must be contiguous float32 [tokens, top_k]");
             return nullptr;
         }
+        if (!status_word(status)) return nullptr;
         if (ws && !ws->is_contiguous()) { fail("workspace must be contiguous"); return nullptr; }
         const int64_t most = 1ll << 31;
         if (tokens >= most || experts >= most || top_k < 0 || top_k >= most || hidden >= most || inner >= most) { fail("too large"); return nullptr; }
-        if (!stream_arg(a[12], &st)) return nullptr;
+        if (!stream_arg(a[13], &st)) return nullptr;
         // the stride of a dimension of one element is whatever torch says: 0 suits every check
         const auto stride = [](const at::Tensor *t, int64_t d, int64_t one) { return t->size(d) == 1 ? one : t->stride(d); };
         sqnn_moe L = {};
@@ -419,12 +420,13 @@ PyObject *moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         void *const p_y = ptr<void>(y), *const p_ws = ptr<void>(ws);
         int32_t *const p_ids = ptr<int32_t>(ids);
         float *const p_probs = ptr<float>(probs);
+        uint32_t *const p_status = ptr<uint32_t>(status);
         const int64_t ldx = row_stride(x), ldy = row_stride(y);
         const size_t ws_bytes = bytes_of(ws);
         int rc;
         {
             Unlocked u;
-            rc = f_moe_fp8(&L, (uint32_t)tokens, p_x, xt, ldx, p_y, yt, ldy, p_ids, p_probs, p_ws, ws_bytes, st);
+            rc = f_moe_fp8(&L, (uint32_t)tokens, p_x, xt, ldx, p_y, yt, ldy, p_ids, p_probs, p_ws, ws_bytes, p_status, st);
         }
         return PyLong_FromLong(rc);
     });

@@ -20,7 +20,7 @@ LIB_PATH = os.environ.get("SQNN_LIBRARY") or os.path.join(_HERE, "libsqnn.so")
 
 MAX_PLANES = 8
 FP8_BLOCK = 128
-MOE_MAX_TOKENS, MOE_MAX_EXPERTS, MOE_MAX_TOP_K, MOE_MAX_LOGITS = 64, 512, 16, 16384
+MOE_MAX_TOKENS, MOE_MAX_EXPERTS, MOE_MAX_TOP_K, MOE_MAX_LOGITS, MOE_MAX_WIDTH = 64, 512, 16, 16384, 14336
 STATIC_SCRATCH_BYTES = 8 << 20
 OUT_BITS, OUT_BF16, OUT_SINK = 0, 1, 2
 X_F32, X_BF16 = 0, 1
@@ -136,7 +136,7 @@ def lib():
         L.sqnn_rmsnorm_fp8.restype = i32
         L.sqnn_fp8_matmul.argtypes = [u64, u64, u32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, i64, vp, vp]
         L.sqnn_fp8_matmul.restype = i32
-        L.sqnn_moe_fp8.argtypes = [P(Moe), u32, vp, i32, i64, vp, i32, i64, vp, vp, vp, sz, vp]
+        L.sqnn_moe_fp8.argtypes = [P(Moe), u32, vp, i32, i64, vp, i32, i64, vp, vp, vp, sz, vp, vp]
         L.sqnn_moe_fp8.restype = i32
         L.sqnn_moe_workspace_bytes.argtypes = [u32, u32, u32]
         L.sqnn_moe_workspace_bytes.restype = sz
@@ -360,7 +360,8 @@ def sqnn_store_probe(d_out, chunk_bytes: int = 3200, stream=None):
 
 def sqnn_set_debug_flags(flags: int, wait_limit_cycles: int = 0) -> None:
     """Test knob: bit 0 = the large-batch kernel's loader issues no loads, bit 1 = the small-batch kernel's MMA
-    warps report no completion, bit 2 = the walk over care bits issues no bulk copies, bit 3 = the 8-bit product's loader issues no loads; wait_limit_cycles bounds their waits."""
+    warps report no completion, bit 2 = the walk over care bits issues no bulk copies, bit 3 = the 8-bit product's loader issues no loads, bit 4 = those of the
+    mixture-of-experts layer; wait_limit_cycles bounds their waits."""
     lib().sqnn_set_debug_flags(int(flags), int(wait_limit_cycles))
 
 
@@ -414,7 +415,7 @@ def sqnn_moe_workspace_bytes(tokens: int, top_k: int, inner: int) -> int:
 
 
 def sqnn_moe_fp8(d_x, d_router, top_k: int, renormalize: bool, d_gate_up, d_gate_up_scale, d_down, d_down_scale, d_y, d_workspace,
-                 d_ids=None, d_probs=None, stream=None):
+                 d_ids=None, d_probs=None, d_status=None, stream=None):
     """A mixture-of-experts layer for up to ``MOE_MAX_TOKENS`` tokens: the ``top_k`` experts with the largest d_x . d_router (equal ones:
     the lowest index), and y = sum of their shares times D (silu(G x) * (U x)).  d_x: [tokens, hidden] and d_router: [experts, hidden],
     float32 or bfloat16 alike; d_gate_up: float8_e4m3fn [experts, 2, inner, hidden] (G, then U) with d_gate_up_scale float32
@@ -423,6 +424,6 @@ def sqnn_moe_fp8(d_x, d_router, top_k: int, renormalize: bool, d_gate_up, d_gate
     d_workspace: ``sqnn_moe_workspace_bytes`` bytes; d_ids int32 and d_probs float32 [tokens, top_k] get the choice (may be None).
     ``renormalize``: the shares of the chosen experts sum to 1.  Queues on ``stream``; does not synchronise."""
     status = (_native_module or _native()).moe_fp8(d_x, d_router, top_k, renormalize, d_gate_up, d_gate_up_scale, d_down, d_down_scale, d_y,
-                                                   d_workspace, d_ids, d_probs, stream)
+                                                   d_workspace, d_ids, d_probs, d_status, stream)
     if status:
         raise SqnnError(status, "sqnn_moe_fp8")

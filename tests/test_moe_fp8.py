@@ -209,6 +209,25 @@ def test_own_stream_graph_and_two_at_once():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("tokens,experts,hidden,inner", [(1, 4, 512, 256), (20, 8, 3500, 700)])
+def test_a_wait_that_gives_up_ends_the_call(tokens, experts, hidden, inner):
+    lay, x = layer(experts, hidden, inner, F32, 21), tokens_of(tokens, hidden, F32, 22)
+    good = call(x, lay, 2)
+    router, gu, gus, down, ds = lay
+    y, status = torch.zeros_like(x), torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.zeros(sqnn.sqnn_moe_workspace_bytes(tokens, 2, inner), dtype=torch.uint8, device="cuda")
+    sqnn.sqnn_set_debug_flags(16, 2_000_000)
+    try:
+        sqnn.sqnn_moe_fp8(x, router, 2, True, gu, gus, down, ds, y, ws, None, None, status)
+        torch.cuda.synchronize()
+    finally:
+        sqnn.sqnn_set_debug_flags(0, 0)
+    assert int(status.item()) == -sqnn.E_TIMEOUT
+    assert bool((y == 0).all())
+    assert all(torch.equal(a, b) for a, b in zip(call(x, lay, 2), good))       # the next call is not affected
+
+
+@pytest.mark.gpu
 def test_norm_then_layer():
     lay = layer(10, 768, 256, BF16, 19)
     g = torch.Generator().manual_seed(20)
@@ -231,9 +250,9 @@ def test_refusals_of_the_c_entry_point():
     ok = dict(tokens=4, x=4096, xt=0, ldx=256, y=8192, yt=0, ldy=256, ids=None, probs=None, ws=65536, bytes=1 << 20)
 
     def rc(lay=None, **changed):
-        return f(ctypes.byref(lay or c_layer()), *{**ok, **changed}.values(), None)
+        return f(ctypes.byref(lay or c_layer()), *{**ok, **changed}.values(), None, None)
 
-    assert f(None, *ok.values(), None) == sqnn.E_INVALID_ARG
+    assert f(None, *ok.values(), None, None) == sqnn.E_INVALID_ARG
     for bad in (dict(tokens=0), dict(x=None), dict(y=None), dict(xt=2), dict(yt=-1), dict(ldx=255), dict(ldy=255), dict(x=4098), dict(y=8193, yt=1), dict(ids=4097),
                 dict(probs=4098)):
         assert rc(**bad) == sqnn.E_INVALID_ARG, bad
@@ -241,7 +260,7 @@ def test_refusals_of_the_c_entry_point():
                 dict(down=None), dict(down_scale=None), dict(router_row=255), dict(gate_up_row=240), dict(down_row=112), dict(gate_up_half=-16),
                 dict(gate_up_expert=-16), dict(down_expert=-16), dict(gate_up_scale=4098), dict(down_scale=4097), dict(router=4097)):
         assert rc(c_layer(**bad)) == sqnn.E_INVALID_ARG, bad
-    for bad in (dict(experts=513), dict(top_k=17, experts=32), dict(gate_up=4104), dict(down=4100), dict(gate_up_row=264), dict(down_row=136),
+    for bad in (dict(experts=513), dict(top_k=17, experts=32), dict(gate_up=4104), dict(down=4100), dict(gate_up_row=264), dict(down_row=136), dict(gate_up_half=32784), dict(gate_up_expert=65600), dict(down_expert=32784),
                 dict(hidden=(1 << 20) + 1, router_row=1 << 21, gate_up_row=1 << 21), dict(inner=(1 << 20) + 1, down_row=1 << 21)):
         lay = c_layer(**bad)
         assert rc(lay, ldx=1 << 21, ldy=1 << 21) == sqnn.E_UNSUPPORTED, bad
