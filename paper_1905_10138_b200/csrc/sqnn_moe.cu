@@ -35,8 +35,9 @@
 namespace sqnn {
 namespace {
 
-constexpr uint32_t WARPS = 16, THREADS = WARPS * 32;              // first kernel; the second has STREAMS warps
-constexpr uint32_t STREAMS = 8;           // warps that stream weights
+constexpr uint32_t WARPS = 16, THREADS = WARPS * 32;              // first kernel
+constexpr uint32_t STREAMS = 8;           // its warps that stream weights
+constexpr uint32_t DOWN_WARPS = 12;       // second kernel: all stream
 constexpr uint32_t CLUSTER = 4;           // CTAs that share the routing's work
 constexpr uint32_t STEP = FP8_BLOCK;      // columns per step of a warp
 constexpr uint32_t GROUP = 8;             // tokens multiplied together
@@ -50,6 +51,7 @@ constexpr uint32_t H_BLOCK = 2 * 2 * STEP + 4 * (STEP / 16);      // inner value
 constexpr uint32_t H_PITCH = H_BLOCK + 16;                        // the same in shared memory: neighbouring tokens in other banks
 constexpr uint32_t MAX_DOWN_DEPTH = 8;
 constexpr uint64_t WAIT_LIMIT_CYCLES = 4000000000ull;
+constexpr uint32_t ALL = 0xffffffffu;
 
 // An entry of the list of chosen experts, as the second kernel needs it.
 struct Entry {
@@ -86,46 +88,16 @@ struct MoeArgs {
 
 struct Routing {
     int32_t ids[MAX_PAIRS];
-    float probs[MAX_PAIRS];
+    float probs[MAX_PAIRS];               // before they are divided
     uint32_t mask[MAX_EXPERTS][2];        // tokens of an expert
     uint32_t entry[MAX_ENTRIES];          // expert | group of tokens << 16
     uint32_t totals[WARPS];
     uint32_t entries;
-    uint32_t exponent[MAX_TOKENS];        // biased, of a token's largest activation
+    uint32_t largest[MAX_TOKENS];         // magnitude of a token's largest activation, as bits
+    float total[MAX_TOKENS];              // what its shares are divided by
 };
 constexpr uint32_t ROUTING_BYTES = (sizeof(Routing) + 127) / 128 * 128;
 
-// From ids to the list of (expert, group of up to `per` of its tokens), ascending.  All threads; ends with a barrier.
-SQNN_DEV void list_entries(Routing &R, const MoeArgs &M, uint32_t per)
-{
-    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    for (uint32_t i = tid; i < 2 * M.experts; i += THREADS) (&R.mask[0][0])[i] = 0;
-    __syncthreads();
-    for (uint32_t i = tid; i < M.tokens * M.top_k; i += THREADS) {
-        const uint32_t t = i / M.top_k;
-        atomicOr(&R.mask[R.ids[i]][t >> 5], 1u << (t & 31));
-    }
-    __syncthreads();
-    static_assert(MAX_EXPERTS <= THREADS, "an expert per thread");
-    const uint32_t mine = tid < M.experts ? __popc(R.mask[tid][0]) + __popc(R.mask[tid][1]) : 0, groups = (mine + per - 1) / per;
-    uint32_t sum = groups;
-#pragma unroll
-    for (uint32_t d = 1; d < 32; d <<= 1) {
-        const uint32_t v = __shfl_up_sync(0xffffffffu, sum, d);
-        if (lane >= d) sum += v;
-    }
-    if (lane == 31) R.totals[warp] = sum;
-    __syncthreads();
-    uint32_t before = 0, all = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < WARPS; ++w) {
-        if (w < warp) before += R.totals[w];
-        all += R.totals[w];
-    }
-    for (uint32_t g = 0; g < groups; ++g) R.entry[before + sum - groups + g] = tid | (g << 16);
-    if (tid == 0) R.entries = all;
-    __syncthreads();
-}
 SQNN_DEV uint32_t tokens_of(const Routing &R, uint32_t expert) { return __popc(R.mask[expert][0]) + __popc(R.mask[expert][1]); }
 // The n-th token of an expert, MAX_TOKENS if it has fewer.
 SQNN_DEV uint32_t token_of(const Routing &R, uint32_t expert, uint32_t n)
@@ -147,12 +119,6 @@ SQNN_DEV uint32_t pair_of(const Routing &R, const MoeArgs &M, uint32_t token, ui
 
 // ---- the multiplication of one chunk
 
-SQNN_DEV uint32_t fp8x2_to_f16x2(uint32_t two)
-{
-    uint32_t v;
-    asm("{\n .reg .b16 t;\n cvt.u16.u32 t, %1;\n cvt.rn.f16x2.e4m3x2 %0, t;\n}\n" : "=r"(v) : "r"(two));
-    return v;
-}
 SQNN_DEV uint32_t f16x2(float lo, float hi)
 {
     uint32_t v;
@@ -161,6 +127,11 @@ SQNN_DEV uint32_t f16x2(float lo, float hi)
 }
 SQNN_DEV float f16_lo(uint32_t v) { float f; asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %1;\n cvt.f32.f16 %0, l;\n}\n" : "=f"(f) : "r"(v)); return f; }
 SQNN_DEV float f16_hi(uint32_t v) { float f; asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %1;\n cvt.f32.f16 %0, h;\n}\n" : "=f"(f) : "r"(v)); return f; }
+SQNN_DEV void mma_f16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)     // c = a b
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};\n"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
 SQNN_DEV void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
@@ -203,10 +174,8 @@ SQNN_DEV uint32_t matrix_row(uint32_t lane) { return ((lane & 7) + (lane & 8)) *
 // A operand of an MMA from a lane's four bytes of row g and of row g + 8.
 SQNN_DEV void weights_of(uint32_t (&a)[4], uint32_t top, uint32_t bottom)
 {
-    a[0] = fp8x2_to_f16x2(top);
-    a[1] = fp8x2_to_f16x2(bottom);
-    a[2] = fp8x2_to_f16x2(top >> 16);
-    a[3] = fp8x2_to_f16x2(bottom >> 16);
+    asm("{\n .reg .b16 tl, th, bl, bh;\n mov.b32 {tl, th}, %4;\n mov.b32 {bl, bh}, %5;\n cvt.rn.f16x2.e4m3x2 %0, tl;\n cvt.rn.f16x2.e4m3x2 %1, bl;\n"
+        " cvt.rn.f16x2.e4m3x2 %2, th;\n cvt.rn.f16x2.e4m3x2 %3, bh;\n}\n" : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]) : "r"(top), "r"(bottom));
 }
 
 // ---- routing
@@ -237,103 +206,219 @@ SQNN_DEV void row_values8(const __nv_bfloat16 *row, uint32_t at, uint32_t n, boo
     }
 }
 
-// Logits of this CTA's experts (every CLUSTER-th) into the shared memory of all CTAs of the cluster.  Eight products at a time in fp32,
-// their sums in 64 bits: which experts a token goes to must not hang on the order of a sum.
-template <typename XT>
-SQNN_DEV void logits_of_cluster(const MoeArgs &M, double *logits)
+// Logits of this CTA's experts (every CLUSTER-th) into the shared memory of all CTAs of the cluster, and the tokens' largest
+// activations.  Some products at a time are summed in fp32, these sums in 64 bits: which experts a token goes to must not hang on the order of a sum.
+// `scratch`: 16 KB.
+SQNN_DEV void send_logit(const MoeArgs &M, double *logits, uint32_t token, uint32_t expert, double v)
 {
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = cluster_rank();
+    const uint32_t at = smem_addr(logits + token * M.experts + expert);
+#pragma unroll 1
+    for (uint32_t r = 0; r < CLUSTER; ++r) peer_store(peer_addr(at, r), v);
+}
+
+// 16 bf16 numbers of a row from `at` on, zero from `n` on.
+SQNN_DEV void raw16(const __nv_bfloat16 *row, uint32_t at, uint32_t n, bool vec, uint32_t (&v)[8])
+{
+    if (vec && at + 16 <= n) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(row + at), b = *reinterpret_cast<const uint4 *>(row + at + 8);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+        const uint16_t *const p = reinterpret_cast<const uint16_t *>(row);
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+            v[j] = (at + 2 * j < n ? p[at + 2 * j] : 0u) | (at + 2 * j + 1 < n ? (uint32_t)p[at + 2 * j + 1] << 16 : 0u);
+    }
+}
+
+// bf16: on the tensor cores, 16 experts by 8 tokens by 64 columns (four MMAs, products exact) at a time.  The columns of a tile are shared by as
+// many warps as there are to spare.
+SQNN_DEV void logits_of_cluster(const MoeArgs &M, double *logits, double *scratch, Routing &R, const __nv_bfloat16 *x, const __nv_bfloat16 *router)
+{
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3, rank = cluster_rank();
+    // (a CTA without experts still looks at the tokens)
+    const uint32_t mine = (M.experts - rank + CLUSTER - 1) / CLUSTER, n_tiles = (M.tokens + 7) / 8, tiles = (max(mine, 1u) + 15) / 16 * n_tiles;
+    const uint32_t parts = tiles < WARPS ? WARPS / tiles : 1, steps = (M.hidden + 63) / 64;
+#pragma unroll 1
+    for (uint32_t i = warp; i < tiles * parts; i += WARPS) {
+        const uint32_t tile = i / parts, part = i - tile * parts, e0 = tile / n_tiles * 16, t0 = tile % n_tiles * 8;
+        const __nv_bfloat16 *const ra = router + (int64_t)min(rank + CLUSTER * (e0 + g), M.experts - 1) * M.ldr;
+        const __nv_bfloat16 *const rb = router + (int64_t)min(rank + CLUSTER * (e0 + g + 8), M.experts - 1) * M.ldr;
+        const __nv_bfloat16 *const xr = x + (int64_t)min(t0 + g, M.tokens - 1) * M.ldx;
+        double sum[4] = {};
+        uint32_t top = 0;
+#pragma unroll 2
+        for (uint32_t c = steps * part / parts; c < steps * (part + 1) / parts; ++c) {
+            const uint32_t at = c * 64 + t4 * 16;
+            uint32_t a[8], b[8], v[8];
+            raw16(ra, at, M.hidden, M.r_vec, a);
+            raw16(rb, at, M.hidden, M.r_vec, b);
+            raw16(xr, at, M.hidden, M.x_vec, v);
+            float s[4] = {};
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+                             : "+f"(s[0]), "+f"(s[1]), "+f"(s[2]), "+f"(s[3])
+                             : "r"(a[2 * j]), "r"(b[2 * j]), "r"(a[2 * j + 1]), "r"(b[2 * j + 1]), "r"(v[2 * j]), "r"(v[2 * j + 1]));
+                top = __vmaxu2(top, __vmaxu2(v[2 * j] & 0x7fff7fffu, v[2 * j + 1] & 0x7fff7fffu));
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) sum[j] += (double)s[j];
+        }
+        if (e0 == 0) {
+            top = max(top & 0xffffu, top >> 16) << 16;
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            if (t4 == 0 && t0 + g < M.tokens) atomicMax(&R.largest[t0 + g], top);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t e = e0 + g + (j >> 1) * 8, t = t0 + 2 * t4 + (j & 1);
+            if (parts > 1) scratch[i * 128 + j * 32 + lane] = sum[j];
+            else if (e < mine && t < M.tokens) send_logit(M, logits, t, rank + CLUSTER * e, sum[j]);
+        }
+    }
+    if (parts == 1) return;
+    __syncthreads();
+#pragma unroll 1
+    for (uint32_t i = tid; i < tiles * 128; i += THREADS) {
+        const uint32_t tile = i / 128, j = i / 32 & 3, l = i & 31, e = tile / n_tiles * 16 + (l >> 2) + (j >> 1) * 8, t = tile % n_tiles * 8 + 2 * (l & 3) + (j & 1);
+        double sum = 0.0;
+        for (uint32_t p = 0; p < parts; ++p) sum += scratch[(tile * parts + p) * 128 + (i & 127)];
+        if (e < mine && t < M.tokens) send_logit(M, logits, t, rank + CLUSTER * e, sum);
+    }
+}
+
+// fp32: a warp per expert, four tokens and a share of the columns; eight products at a time.
+SQNN_DEV void logits_of_cluster(const MoeArgs &M, double *logits, double *scratch, Routing &R, const float *x, const float *router)
+{
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank();
     constexpr uint32_t SHARE = 4;                                // tokens that share a read of an expert's row
-    const uint32_t groups = (M.tokens + SHARE - 1) / SHARE, mine = (M.experts - rank + CLUSTER - 1) / CLUSTER;
-    const XT *const x = static_cast<const XT *>(M.x), *const router = static_cast<const XT *>(M.router);
-    for (uint32_t i = warp; i < mine * groups; i += WARPS) {
-        const uint32_t e = rank + CLUSTER * (i / groups), t0 = i % groups * SHARE;
+    const uint32_t mine = (M.experts - rank + CLUSTER - 1) / CLUSTER, groups = (M.tokens + SHARE - 1) / SHARE, tasks = max(mine, 1u) * groups;
+    const uint32_t parts = tasks < WARPS ? WARPS / tasks : 1, steps = (M.hidden + 255) / 256;
+#pragma unroll 1
+    for (uint32_t i = warp; i < tasks * parts; i += WARPS) {
+        const uint32_t task = i / parts, part = i - task * parts, own = task / groups, t0 = task % groups * SHARE;
+        const float *const r_row = router + (int64_t)min(rank + CLUSTER * own, M.experts - 1) * M.ldr;
         double sum[SHARE] = {};
-        for (uint32_t at = lane * 8; at < M.hidden; at += 256) {
+        uint32_t top[SHARE] = {};
+#pragma unroll 2
+        for (uint32_t c = steps * part / parts; c < steps * (part + 1) / parts; ++c) {
+            const uint32_t at = c * 256 + lane * 8;
             float r[8];
-            row_values8(router + (int64_t)e * M.ldr, at, M.hidden, M.r_vec, r);
+            row_values8(r_row, at, M.hidden, M.r_vec, r);
 #pragma unroll
             for (uint32_t t = 0; t < SHARE; ++t) {
-                if (t0 + t < M.tokens) {
-                    float v[8], s = 0.0f;
-                    row_values8(x + (int64_t)(t0 + t) * M.ldx, at, M.hidden, M.x_vec, v);
+                float v[8], s = 0.0f;
+                row_values8(x + (int64_t)min(t0 + t, M.tokens - 1) * M.ldx, at, M.hidden, M.x_vec, v);
 #pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) s = fmaf(r[j], v[j], s);
-                    sum[t] += (double)s;
+                for (uint32_t j = 0; j < 8; ++j) {
+                    s = fmaf(r[j], v[j], s);
+                    top[t] = max(top[t], __float_as_uint(v[j]) & 0x7fffffffu);
                 }
+                sum[t] += (double)s;
             }
         }
 #pragma unroll
         for (uint32_t t = 0; t < SHARE; ++t) {
 #pragma unroll
             for (uint32_t d = 16; d; d >>= 1) sum[t] += __shfl_xor_sync(0xffffffffu, sum[t], d);
-            if (t0 + t < M.tokens && lane < CLUSTER) peer_store(peer_addr(smem_addr(logits + (t0 + t) * M.experts + e), lane), sum[t]);
+            const uint32_t most = __reduce_max_sync(0xffffffffu, top[t]);
+            if (lane == 0 && t0 + t < M.tokens) {
+                if (own == 0) atomicMax(&R.largest[t0 + t], most);
+                if (parts > 1) scratch[i * SHARE + t] = sum[t];
+                else if (own < mine) send_logit(M, logits, t0 + t, rank + CLUSTER * own, sum[t]);
+            }
         }
+    }
+    if (parts == 1) return;
+    __syncthreads();
+    if (tid < tasks * SHARE) {
+        const uint32_t task = tid / SHARE, t = task % groups * SHARE + tid % SHARE;
+        double sum = 0.0;
+        for (uint32_t p = 0; p < parts; ++p) sum += scratch[(task * parts + p) * SHARE + tid % SHARE];
+        if (t < M.tokens && task / groups < mine) send_logit(M, logits, t, rank + CLUSTER * (task / groups), sum);
     }
 }
 
-// The top_k experts of each token and their shares; a warp per token.  NaN counts as the largest, so that there are always top_k different ones.
-SQNN_DEV void choose(const MoeArgs &M, const double *logits, Routing &R)
+// 64-bit floating numbers as integers of the same order; NaN comes last.  And back.
+SQNN_DEV int64_t key_of(double v)
 {
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const double INF = __longlong_as_double(0x7ff0000000000000ll);
-    for (uint32_t t = warp; t < M.tokens; t += WARPS) {
-        const double *l = logits + t * M.experts;
-        uint32_t taken = 0;                                      // bit j: expert lane + 32 j
-        double first = 0.0;
-        float total = 0.0f, mine = 0.0f;                         // lane s keeps the share of the s-th expert
-        for (uint32_t s = 0; s < M.top_k; ++s) {
-            double best = -INF;
-            uint32_t at = MAX_EXPERTS;
-            for (uint32_t j = 0, e = lane; e < M.experts; ++j, e += 32) {
-                if (taken >> j & 1) continue;
-                double v = l[e];
-                v = v != v ? INF : v;
-                if (at == MAX_EXPERTS || v > best) { best = v; at = e; }
-            }
-#pragma unroll
-            for (uint32_t d = 16; d; d >>= 1) {
-                const double v = __shfl_xor_sync(0xffffffffu, best, d);
-                const uint32_t a = __shfl_xor_sync(0xffffffffu, at, d);
-                if (a != MAX_EXPERTS && (at == MAX_EXPERTS || v > best || (v == best && a < at))) { best = v; at = a; }
-            }
-            if ((at & 31) == lane) taken |= 1u << (at >> 5);
-            const double raw = l[at];
-            if (s == 0) first = raw;
-            const float p = expf((float)(raw - first));
-            if (lane == s) { mine = p; R.ids[t * M.top_k + s] = (int32_t)at; }
-            total += p;
+    if (v != v) return 0x7fffffffffffffffll;
+    const int64_t b = __double_as_longlong(v == 0.0 ? 0.0 : v);
+    return b ^ ((b >> 63) & 0x7fffffffffffffffll);
+}
+SQNN_DEV double value_of(int64_t k) { return __longlong_as_double(k ^ ((k >> 63) & 0x7fffffffffffffffll)); }
+
+// From logits to the top_k experts of each token, their shares, and the list of (expert, group of up to `per` of its tokens), ascending.  NaN counts as the
+// largest, so that there are always top_k different experts.  All threads; begins and ends with a barrier.
+SQNN_DEV void choose(const MoeArgs &M, double *logits, Routing &R)
+{
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, all = M.tokens * M.experts, pairs = M.tokens * M.top_k;
+    int64_t *const keys = reinterpret_cast<int64_t *>(logits);
+    __syncthreads();
+    for (uint32_t i = tid; i < all; i += THREADS) keys[i] = key_of(logits[i]);
+    for (uint32_t i = tid; i < 2 * M.experts; i += THREADS) (&R.mask[0][0])[i] = 0;
+    __syncthreads();
+    // an expert's place is the number of those before it; four threads count
+#pragma unroll 1
+    for (uint32_t i0 = 0; i0 < all; i0 += THREADS / 4) {
+        const uint32_t i = i0 + tid / 4, t = min(i, all - 1) / M.experts, e = min(i, all - 1) - t * M.experts;
+        const int64_t mine = keys[t * M.experts + e];
+        uint32_t place = 0;
+#pragma unroll 4
+        for (uint32_t j = tid & 3; j < M.experts; j += 4) place += keys[t * M.experts + j] > mine - (j < e ? 1 : 0) ? 1 : 0;
+        place += __shfl_xor_sync(0xffffffffu, place, 1);
+        place += __shfl_xor_sync(0xffffffffu, place, 2);
+        if (i < all && (tid & 3) == 0 && place < M.top_k) {
+            R.ids[t * M.top_k + place] = (int32_t)e;
+            atomicOr(&R.mask[e][t >> 5], 1u << (t & 31));
         }
-        if (!M.renormalize) {
-            total = 0.0f;
-            for (uint32_t e = lane; e < M.experts; e += 32) total += expf((float)(l[e] - first));
-#pragma unroll
-            for (uint32_t d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-        }
-        if (lane < M.top_k) R.probs[t * M.top_k + lane] = mine / total;
     }
+    __syncthreads();
+    for (uint32_t i = tid; i < pairs; i += THREADS) {
+        const uint32_t t = i / M.top_k;
+        const int64_t *const k = keys + t * M.experts;
+        R.probs[i] = expf((float)(value_of(k[R.ids[i]]) - value_of(k[R.ids[t * M.top_k]])));
+    }
+    static_assert(MAX_EXPERTS <= THREADS, "an expert per thread");
+    const uint32_t groups = tid < M.experts ? (tokens_of(R, tid) + M.per - 1) / M.per : 0;
+    uint32_t upto = groups;
+#pragma unroll
+    for (uint32_t d = 1; d < 32; d <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += v;
+    }
+    if (lane == 31) R.totals[warp] = upto;
+    __syncthreads();
+    if (M.renormalize) {
+        if (tid < M.tokens) {
+            float sum = 0.0f;
+            for (uint32_t s = 0; s < M.top_k; ++s) sum += R.probs[tid * M.top_k + s];
+            R.total[tid] = sum;
+        }
+    } else {
+        for (uint32_t t = warp; t < M.tokens; t += WARPS) {
+            const int64_t *const k = keys + t * M.experts;
+            const double first = value_of(k[R.ids[t * M.top_k]]);
+            float sum = 0.0f;
+            for (uint32_t e = lane; e < M.experts; e += 32) sum += expf((float)(value_of(k[e]) - first));
+#pragma unroll
+            for (uint32_t d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            if (lane == 0) R.total[t] = sum;
+        }
+    }
+    uint32_t before = 0, count = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < WARPS; ++w) {
+        if (w < warp) before += R.totals[w];
+        count += R.totals[w];
+    }
+    for (uint32_t g = 0; g < groups; ++g) R.entry[before + upto - groups + g] = tid | (g << 16);
+    if (tid == 0) R.entries = count;
+    __syncthreads();
 }
 
 // ---- first kernel: routing, then h = silu(G x) * (U x) for every (token, expert)
-
-// Exponents of the tokens' largest activations; a warp per token.
-template <typename XT>
-SQNN_DEV void exponents(const MoeArgs &M, Routing &R)
-{
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (uint32_t t = warp; t < M.tokens; t += WARPS) {
-        const XT *row = static_cast<const XT *>(M.x) + (int64_t)t * M.ldx;
-        uint32_t top = 0;
-        for (uint32_t at = lane * 8; at < M.hidden; at += 256) {
-            float v[8];
-            row_values8(row, at, M.hidden, M.x_vec, v);
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-        }
-        top = __reduce_max_sync(0xffffffffu, top);
-        if (lane == 0) R.exponent[t] = exponent_of(top);
-    }
-}
 
 // A warp's waits: bounded; once one has given up, its block asks for and waits for nothing any more, and stores nothing.
 struct Waits {
@@ -374,21 +459,48 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
     const Waits W{&abort_word, M.status, M.wait_limit};
     if (tid < STREAMS * UP_DEPTH) mbar_init(smem_addr(bars + tid), 1);
     if (tid == 0) abort_word = 0;
+    if (tid < MAX_TOKENS) R.largest[tid] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     wait_prior_grid();
     launch_dependents();
     cluster_sync();                                              // all CTAs of the cluster run: their shared memory may be written
-    logits_of_cluster<XT>(M, logits);
-    exponents<XT>(M, R);
+    logits_of_cluster(M, logits, reinterpret_cast<double *>(parts), R, static_cast<const XT *>(M.x), static_cast<const XT *>(M.router));
     cluster_sync();                                              // (the last time that one CTA writes to another)
+    // Tokens, scaled and in fp16, to rows `base` and on: an expert's, from the first-th on, or all.
+    const uint32_t steps = (M.hidden + STEP - 1) / STEP, lo_at = steps * STEP * 2;
+    auto stage = [&](uint32_t base, uint32_t count, uint32_t expert, uint32_t first) {
+        const uint32_t cols8 = steps * (STEP / 8);
+        for (uint32_t i = tid; i < count * cols8; i += THREADS) {
+            const uint32_t k = i / cols8, at = (i - k * cols8) * 8, t = expert == ALL ? k : token_of(R, expert, first + k);
+            const float s = scale_of(exponent_of(R.largest[t]));
+            float v[8];
+            row_values8(static_cast<const XT *>(M.x) + (int64_t)t * M.ldx, at, M.hidden, M.x_vec, v);
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                const float a = v[2 * j] * s, b = v[2 * j + 1] * s;
+                hi[j] = f16x2(a, b);
+                lo[j] = f16x2(a - f16_lo(hi[j]), b - f16_hi(hi[j]));
+            }
+            // columns 16 j + 4 t and on, t even: four at position 16 t + 4 j, the next four at 16 (t + 1) + 4 j
+            uint8_t *const p = x_rows + (base + k) * M.x_row + (at & ~63u) * 2 + (at & 12u) * 8 + (at >> 4 & 3u) * 8;
+            *reinterpret_cast<uint2 *>(p) = make_uint2(hi[0], hi[1]);
+            *reinterpret_cast<uint2 *>(p + 32) = make_uint2(hi[2], hi[3]);
+            if constexpr (PIECES == 2) {
+                *reinterpret_cast<uint2 *>(p + lo_at) = make_uint2(lo[0], lo[1]);
+                *reinterpret_cast<uint2 *>(p + lo_at + 32) = make_uint2(lo[2], lo[3]);
+            }
+        }
+    };
+    const bool early = M.tokens <= M.x_rows;                     // there is room for all tokens: a row each, once and for all
+    if (early) stage(0, M.tokens, ALL, 0);
     choose(M, logits, R);
     fence_async_smem();                                          // the rings' copies come after what was read and written here
     __syncthreads();
-    list_entries(R, M, M.per);
     if (blockIdx.x == 0) {                                       // for the caller and for the second kernel
         for (uint32_t i = tid; i < M.tokens * M.top_k; i += THREADS) {
             if (M.ids_out) M.ids_out[i] = R.ids[i];
-            if (M.probs_out) M.probs_out[i] = R.probs[i];
+            if (M.probs_out) M.probs_out[i] = R.probs[i] / R.total[i / M.top_k];
         }
         for (uint32_t i = tid; i < R.entries * GROUP; i += THREADS) {
             const uint32_t n = i / GROUP, k = i % GROUP, en = R.entry[n], e = en & 0xffffu, first = (en >> 16) * M.per, count = min(M.per, tokens_of(R, e) - first);
@@ -398,14 +510,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
                 const uint32_t t = token_of(R, e, first + k), pair = pair_of(R, M, t, e);
                 E.token[k] = t;
                 E.pair[k] = pair;
-                E.prob[k] = R.probs[pair];
+                E.prob[k] = R.probs[pair] / R.total[t];
             }
         }
         if (tid == 0) *M.list_size = R.entries;
     }
 
-    const uint32_t per_entry = (M.inner + 15) / 16, units = R.entries * per_entry, steps = (M.hidden + STEP - 1) / STEP;
-    const uint32_t u0 = (uint32_t)((uint64_t)units * blockIdx.x / gridDim.x), u1 = (uint32_t)((uint64_t)units * (blockIdx.x + 1) / gridDim.x);
+    const uint32_t per_entry = (M.inner + 15) / 16, units = R.entries * per_entry;     // (below 2^21)
+    const uint32_t u0 = units * blockIdx.x / gridDim.x, u1 = units * (blockIdx.x + 1) / gridDim.x;
     const uint32_t iblocks = (M.inner + FP8_BLOCK - 1) / FP8_BLOCK;
     auto tokens_in = [&](uint32_t n) {                           // of entry n
         const uint32_t en = R.entry[n];
@@ -417,9 +529,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
         if (round0 >= u1) return;
         if (round0 >= w.window1) {
             uint32_t n = round0 / per_entry, rows = 0;
-            while (n < R.entries && n * per_entry < u1 && rows + tokens_in(n) <= M.x_rows) rows += tokens_in(n++);
+            while (!early && n < R.entries && n * per_entry < u1 && rows + tokens_in(n) <= M.x_rows) rows += tokens_in(n++);
             w.window0 = round0;
-            w.window1 = min(u1, n * per_entry);
+            w.window1 = early ? u1 : min(u1, n * per_entry);
         }
         w.round_n = min(STREAMS, w.window1 - round0);
         if (warp >= STREAMS) return;
@@ -469,13 +581,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
     Walk w;
     w.window1 = w.round_n = 0;
     uint32_t get_slot = 0, get_parity = 0;
-    const uint32_t row_at = matrix_row(lane), lo_at = steps * STEP * 2;
+    const uint32_t row_at = matrix_row(lane);
     const float *unit_scale = nullptr;                           // the unit's scales of G; those of U `to_up` further on
     const uint64_t to_up = (uint64_t)iblocks * steps;
-    float next_sg = 0.0f, next_su = 0.0f;                        // asked for a step before they are needed
+    uint32_t next_sg = 0, next_su = 0;                           // asked for a step before they are needed
     auto ask_scales = [&]() {
-        next_sg = __ldg(unit_scale + w.c);
-        next_su = __ldg(unit_scale + to_up + w.c);
+        next_sg = ldg_ahead(reinterpret_cast<const uint32_t *>(unit_scale + w.c));
+        next_su = ldg_ahead(reinterpret_cast<const uint32_t *>(unit_scale + to_up + w.c));
     };
     auto scales_of_unit = [&]() {
         const uint32_t n = w.u / per_entry, e = R.entry[n] & 0xffffu, q = w.u - n * per_entry;
@@ -487,32 +599,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
         const bool fresh = round0 >= w.window1;
         enter(w, round0);
         if (w.left) scales_of_unit();
-        if (fresh) {                                             // the window's tokens, scaled and in fp16
-            const uint32_t n0 = w.window0 / per_entry, n1 = (w.window1 + per_entry - 1) / per_entry, cols8 = steps * (STEP / 8);
+        if (fresh && !early) {                                   // the window's tokens
+            const uint32_t n1 = (w.window1 + per_entry - 1) / per_entry;
             uint32_t base = 0;
-            for (uint32_t n = n0; n < n1; ++n) {
-                const uint32_t en = R.entry[n], e = en & 0xffffu, count = tokens_in(n);
-                for (uint32_t i = tid; i < count * cols8; i += THREADS) {
-                    const uint32_t k = i / cols8, at = (i - k * cols8) * 8, t = token_of(R, e, (en >> 16) * M.per + k);
-                    const float s = scale_of(R.exponent[t]);
-                    float v[8];
-                    row_values8(static_cast<const XT *>(M.x) + (int64_t)t * M.ldx, at, M.hidden, M.x_vec, v);
-                    uint32_t hi[4], lo[4];
-#pragma unroll
-                    for (uint32_t j = 0; j < 4; ++j) {
-                        const float a = v[2 * j] * s, b = v[2 * j + 1] * s;
-                        hi[j] = f16x2(a, b);
-                        lo[j] = f16x2(a - f16_lo(hi[j]), b - f16_hi(hi[j]));
-                    }
-                    // columns 16 j + 4 t and on, t even: four at position 16 t + 4 j, the next four at 16 (t + 1) + 4 j
-                    uint8_t *const p = x_rows + (base + k) * M.x_row + (at & ~63u) * 2 + (at & 12u) * 8 + (at >> 4 & 3u) * 8;
-                    *reinterpret_cast<uint2 *>(p) = make_uint2(hi[0], hi[1]);
-                    *reinterpret_cast<uint2 *>(p + 32) = make_uint2(hi[2], hi[3]);
-                    if constexpr (PIECES == 2) {
-                        *reinterpret_cast<uint2 *>(p + lo_at) = make_uint2(lo[0], lo[1]);
-                        *reinterpret_cast<uint2 *>(p + lo_at + 32) = make_uint2(lo[2], lo[3]);
-                    }
-                }
+            for (uint32_t n = w.window0 / per_entry; n < n1; ++n) {
+                const uint32_t en = R.entry[n], count = tokens_in(n);
+                stage(base, count, en & 0xffffu, (en >> 16) * M.per);
                 base += count;
             }
             __syncthreads();
@@ -525,24 +617,24 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
             float b0 = 0.0f, b1 = 0.0f;
             auto begin = [&]() {                                 // where the tokens of the unit's entry are, and their scales
                 const uint32_t n0 = w.window0 / per_entry, n = w.u / per_entry, en = R.entry[n], e = en & 0xffffu, first = (en >> 16) * M.per, count = tokens_in(n);
-                uint32_t base = 0;
-                for (uint32_t k = n0; k < n; ++k) base += tokens_in(k);
-                x_at = smem_addr(x_rows) + (base + min(g, count - 1)) * M.x_row + t4 * 32;   // columns without a token repeat the last one; nobody looks at them
-                b0 = back_of(R.exponent[token_of(R, e, first + min(2 * t4, count - 1))]);
-                b1 = back_of(R.exponent[token_of(R, e, first + min(2 * t4 + 1, count - 1))]);
+                uint32_t row = early ? token_of(R, e, first + min(g, count - 1)) : min(g, count - 1);
+                for (uint32_t k = n0; k < n && !early; ++k) row += tokens_in(k);
+                x_at = smem_addr(x_rows) + row * M.x_row + t4 * 32;                          // columns without a token repeat the last one; nobody looks at them
+                b0 = back_of(exponent_of(R.largest[token_of(R, e, first + min(2 * t4, count - 1))]));
+                b1 = back_of(exponent_of(R.largest[token_of(R, e, first + min(2 * t4 + 1, count - 1))]));
             };
             if (w.left) begin();
 #pragma unroll 1
             while (w.left) {
                 W.wait(my_bars + 8 * get_slot, get_parity);
                 const uint32_t sa = ring + get_slot * UP_SLOT + row_at, xa = x_at + w.c * (STEP * 2);
-                const float sg = next_sg, su = next_su;
+                const float sg = __uint_as_float(settle(next_sg)), su = __uint_as_float(settle(next_su));
                 bool end = --w.left == 0;
                 const uint32_t unit = w.u;
                 if (++w.c == steps) { w.c = 0; ++w.u; end = true; }
                 if (!end) ask_scales();
                 else if (w.left) scales_of_unit();
-                float cg[2][4] = {}, cu[2][4] = {};
+                float cg[2][4], cu[2][4];
 #pragma unroll
                 for (uint32_t p = 0; p < 4; ++p) {               // 32 columns
                     const uint4 hi = shared16(xa + (p >> 1) * 128 + (p & 1) * 16);
@@ -551,10 +643,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
                     const uint4 wg = matrices((sa) ^ (p << 5)), wu = matrices((sa + UP_SLOT / 2) ^ (p << 5));
                     uint32_t a[4];
                     weights_of(a, wg.x, wg.y);
-                    mma_f16(cg[p & 1], a, hi.x, hi.y);
+                    if (p < 2) mma_f16_first(cg[p & 1], a, hi.x, hi.y);
+                    else mma_f16(cg[p & 1], a, hi.x, hi.y);
                     if constexpr (PIECES == 2) mma_f16(cg[p & 1], a, lo.x, lo.y);
                     weights_of(a, wu.x, wu.y);
-                    mma_f16(cu[p & 1], a, hi.x, hi.y);
+                    if (p < 2) mma_f16_first(cu[p & 1], a, hi.x, hi.y);
+                    else mma_f16(cu[p & 1], a, hi.x, hi.y);
                     if constexpr (PIECES == 2) mma_f16(cu[p & 1], a, lo.x, lo.y);
                     weights_of(a, wg.z, wg.w);
                     mma_f16(cg[p & 1], a, hi.z, hi.w);
@@ -639,18 +733,18 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
 // ---- second kernel: y = sum p D h
 
 template <uint32_t ROWS>
-__global__ void __launch_bounds__(STREAMS * 32, 1) k_moe_down(const __grid_constant__ CUtensorMap weights, const MoeArgs M)
+__global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_constant__ CUtensorMap weights, const MoeArgs M)
 {
     constexpr uint32_t TILES = ROWS / 16, W_BYTES = ROWS * STEP;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    __shared__ uint64_t bars[STREAMS * MAX_DOWN_DEPTH];
+    __shared__ uint64_t bars[DOWN_WARPS * MAX_DOWN_DEPTH];
     __shared__ uint32_t abort_word;
     // [ring of weights][ring of inner values][sums: warp, token, row]
     const uint32_t skew = (1024u - (smem_addr(smem_raw) & 1023u)) & 1023u, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
     uint8_t *const smem = smem_raw + skew;
     const uint32_t h_slot = M.slot - W_BYTES, ring = smem_addr(smem) + warp * M.depth * W_BYTES;
-    const uint32_t h_ring = smem_addr(smem) + STREAMS * M.depth * W_BYTES + warp * M.depth * h_slot, my_bars = smem_addr(bars) + 8 * warp * MAX_DOWN_DEPTH;
-    float *const sums = reinterpret_cast<float *>(smem + (size_t)STREAMS * M.depth * M.slot);
+    const uint32_t h_ring = smem_addr(smem) + DOWN_WARPS * M.depth * W_BYTES + warp * M.depth * h_slot, my_bars = smem_addr(bars) + 8 * warp * MAX_DOWN_DEPTH;
+    float *const sums = reinterpret_cast<float *>(smem + (size_t)DOWN_WARPS * M.depth * M.slot);
     float *const mine = sums + warp * M.tokens * ROWS;
     const uint32_t row0 = blockIdx.x * ROWS;
     const Waits W{&abort_word, M.status, M.wait_limit};
@@ -663,7 +757,7 @@ __global__ void __launch_bounds__(STREAMS * 32, 1) k_moe_down(const __grid_const
     launch_dependents();
     asm volatile("fence.proxy.async.global;\n" ::: "memory");    // the copies below read what the first kernel stored
     const uint32_t steps = (M.inner + STEP - 1) / STEP, total = *M.list_size * steps;
-    const uint32_t q0 = (uint32_t)((uint64_t)total * warp / STREAMS), q1 = (uint32_t)((uint64_t)total * (warp + 1) / STREAMS);
+    const uint32_t q0 = total * warp / DOWN_WARPS, q1 = total * (warp + 1) / DOWN_WARPS;
 
     // ---- a step's weights and its tokens' inner values into the rings
     uint32_t ahead_n = q0 / steps, ahead_c = q0 - ahead_n * steps, ahead_q = q0, put_slot = 0, issued = 0;
@@ -705,7 +799,7 @@ __global__ void __launch_bounds__(STREAMS * 32, 1) k_moe_down(const __grid_const
     // of the entry at hand and of the next one; D's scale is asked for a step before it is needed
     uint32_t next_expert = 0, next_count = 0;
     const float *entry_scale = nullptr;
-    float next_s = 0.0f;
+    uint32_t next_s = 0;
     auto scales_of = [&](uint32_t expert) { return M.down_scale + ((uint64_t)expert * ((M.hidden + FP8_BLOCK - 1) / FP8_BLOCK) + row0 / FP8_BLOCK) * steps; };
     auto look_ahead = [&]() {
         if ((uint64_t)(n + 1) * steps < q1) {
@@ -716,7 +810,7 @@ __global__ void __launch_bounds__(STREAMS * 32, 1) k_moe_down(const __grid_const
     if (q0 < q1) {
         count = M.list[n].count;
         entry_scale = scales_of(M.list[n].expert);
-        next_s = __ldg(entry_scale + c_at);
+        next_s = ldg_ahead(reinterpret_cast<const uint32_t *>(entry_scale + c_at));
         look_ahead();
     }
 #pragma unroll 1
@@ -724,9 +818,10 @@ __global__ void __launch_bounds__(STREAMS * 32, 1) k_moe_down(const __grid_const
         W.wait(my_bars + 8 * get_slot, get_parity);
         const uint32_t sa = ring + get_slot * W_BYTES + row_at, b = h_ring + get_slot * h_slot + min(g, count - 1) * H_PITCH + t4 * 32;
         const uint32_t f_at = h_ring + get_slot * h_slot + 512, f0_at = f_at + min(2 * t4, count - 1) * H_PITCH, f1_at = f_at + min(2 * t4 + 1, count - 1) * H_PITCH;
-        const float s = next_s;
-        if (c_at + 1 < steps) next_s = __ldg(entry_scale + c_at + 1);
-        else if (q + 1 < q1) next_s = __ldg(entry_scale = scales_of(next_expert));
+        const float s = __uint_as_float(settle(next_s));
+        if (c_at + 1 == steps) entry_scale = scales_of(next_expert) - steps;
+        if (q + 1 < q1) next_s = ldg_ahead(reinterpret_cast<const uint32_t *>(entry_scale + c_at + 1));
+        if (c_at + 1 == steps) entry_scale += steps;
         float part[TILES][4] = {};                               // of this step, before D's scale
 #pragma unroll
         for (uint32_t p = 0; p < 4; ++p) {                       // 32 columns
@@ -739,8 +834,8 @@ __global__ void __launch_bounds__(STREAMS * 32, 1) k_moe_down(const __grid_const
                 for (uint32_t j = 0; j < 2; ++j) {
                     uint32_t a[4];
                     weights_of(a, j ? w.z : w.x, j ? w.w : w.y);
-                    float c[4] = {};
-                    mma_f16(c, a, j ? hi.z : hi.x, j ? hi.w : hi.y);
+                    float c[4];
+                    mma_f16_first(c, a, j ? hi.z : hi.x, j ? hi.w : hi.y);
                     mma_f16(c, a, j ? lo.z : lo.x, j ? lo.w : lo.y);
                     part[r][0] = fmaf(c[0], f0[j], part[r][0]);
                     part[r][1] = fmaf(c[1], f1[j], part[r][1]);
@@ -789,11 +884,11 @@ __global__ void __launch_bounds__(STREAMS * 32, 1) k_moe_down(const __grid_const
             }
         return;
     }
-    for (uint32_t i = tid; i < M.tokens * ROWS; i += STREAMS * 32) {
+    for (uint32_t i = tid; i < M.tokens * ROWS; i += DOWN_WARPS * 32) {
         const uint32_t t = i / ROWS, row = row0 + i % ROWS;
         float s = 0.0f;
 #pragma unroll
-        for (uint32_t w = 0; w < STREAMS; ++w) s += sums[w * M.tokens * ROWS + i];
+        for (uint32_t w = 0; w < DOWN_WARPS; ++w) s += sums[w * M.tokens * ROWS + i];
         if (row < M.hidden) {
             const int64_t at = (int64_t)t * M.ldy + row;
             if (M.y_bf16) static_cast<__nv_bfloat16 *>(M.y)[at] = __float2bfloat16_rn(s);
@@ -840,10 +935,10 @@ int launch_moe(MoeArgs M, const sqnn_moe *L, cudaStream_t st)
     // second kernel: 32 rows per CTA where that still makes two CTAs for three SMs; as deep a ring as there is room for
     const uint32_t rows = 3 * ((M.hidden + 31) / 32) >= 2 * (uint32_t)sm_count() ? 32 : 16;
     M.slot = rows * STEP + (M.tokens < M.per ? M.tokens : M.per) * H_PITCH;
-    const size_t sums = (size_t)STREAMS * M.tokens * rows * 4;
-    M.depth = (uint32_t)((SMEM_BYTES - 1024 - sums) / (STREAMS * M.slot));
+    const size_t sums = (size_t)DOWN_WARPS * M.tokens * rows * 4;
+    M.depth = (uint32_t)((SMEM_BYTES - 1024 - sums) / (DOWN_WARPS * M.slot));
     M.depth = M.depth < MAX_DOWN_DEPTH ? M.depth : MAX_DOWN_DEPTH;
-    const size_t smem_down = 1024 + sums + (size_t)STREAMS * M.depth * M.slot;
+    const size_t smem_down = 1024 + sums + (size_t)DOWN_WARPS * M.depth * M.slot;
     CUtensorMap gu_map, d_map;
     if (!make_map(&gu_map, L->gate_up, M.hidden, (uint64_t)(M.experts - 1) * M.gu_expert + M.gu_half + M.inner, L->gate_up_row, 16) ||
         !make_map(&d_map, L->down, M.inner, (uint64_t)(M.experts - 1) * M.d_expert + M.hidden, L->down_row, rows))
@@ -874,7 +969,7 @@ int launch_moe(MoeArgs M, const sqnn_moe *L, cudaStream_t st)
     cfg.gridDim = dim3((uint32_t)clusters * CLUSTER);
     cfg.numAttrs = 2;
     if (cudaLaunchKernelEx(&cfg, up, gu_map, M) != cudaSuccess) return SQNN_E_CUDA;
-    return launch_kernel(rows == 32 ? k_moe_down<32> : k_moe_down<16>, (M.hidden + rows - 1) / rows, STREAMS * 32, smem_down, st, d_map, M);
+    return launch_kernel(rows == 32 ? k_moe_down<32> : k_moe_down<16>, (M.hidden + rows - 1) / rows, DOWN_WARPS * 32, smem_down, st, d_map, M);
 }
 
 int moe_queue(const sqnn_moe *L, uint32_t tokens, const void *d_x, int x_dtype, int64_t ldx, void *d_y, int y_dtype, int64_t ldy,
