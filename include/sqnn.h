@@ -402,7 +402,7 @@ int sqnn_fp8_matmul(uint64_t m, uint64_t n, uint32_t batch, const uint8_t *d_w, 
 #define SQNN_MOE_MAX_EXPERTS 512
 #define SQNN_MOE_MAX_TOP_K   16
 #define SQNN_MOE_MAX_LOGITS  16384     /* tokens x experts */
-#define SQNN_MOE_MAX_WIDTH   14336     /* hidden, inner    */
+#define SQNN_MOE_MAX_WIDTH   11264     /* hidden, inner    */
 
 /* A mixture-of-experts layer in 8 bits.  router: experts rows of `hidden` elements (of the activations' type, row stride
  * router_row).  gate_up: for each expert G then U, `inner` rows of `hidden` e4m3 numbers each (strides: gate_up_expert, gate_up_half from G to U,

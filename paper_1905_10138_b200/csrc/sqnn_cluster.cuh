@@ -5,9 +5,12 @@
 namespace sqnn {
 
 SQNN_DEV uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(r)); return r; }
+SQNN_DEV void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory"); }
+SQNN_DEV void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory"); }
 SQNN_DEV void cluster_sync()
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 SQNN_DEV uint32_t peer_addr(uint32_t sa, uint32_t rank)
 {
@@ -28,9 +31,9 @@ SQNN_DEV uint32_t peer_load(uint32_t a)
     return v;
 }
 
-SQNN_DEV void peer_store(uint32_t a, double v)
+SQNN_DEV void peer_store(uint32_t a, int64_t v)
 {
-    asm volatile("st.shared::cluster.f64 [%0], %1;\n" :: "r"(a), "d"(v) : "memory");
+    asm volatile("st.shared::cluster.s64 [%0], %1;\n" :: "r"(a), "l"(v) : "memory");
 }
 
 }  // namespace sqnn

@@ -44,7 +44,7 @@ constexpr uint32_t GROUP = 8;             // tokens multiplied together
 constexpr uint32_t MAX_TOKENS = SQNN_MOE_MAX_TOKENS, MAX_EXPERTS = SQNN_MOE_MAX_EXPERTS, MAX_TOP_K = SQNN_MOE_MAX_TOP_K;
 constexpr uint32_t MAX_PAIRS = MAX_TOKENS * MAX_TOP_K;
 constexpr uint32_t MAX_ENTRIES = MAX_EXPERTS + MAX_PAIRS;         // chosen experts, those with many tokens several times
-constexpr size_t SMEM_BYTES = 224 * 1024;
+constexpr size_t SMEM_BYTES = 224 * 1024, DOWN_SMEM_BYTES = 216 * 1024;    // (the second kernel has 8 KB of static variables)
 constexpr uint32_t UP_DEPTH = 4, UP_SLOT = 2 * 16 * STEP;         // first kernel's ring: 16 rows of G and of U
 constexpr uint32_t PARTS_BYTES = STREAMS * 2 * 8 * 32 * 4;        // [warp][its first or second unit][sum][lane]
 constexpr uint32_t H_BLOCK = 2 * 2 * STEP + 4 * (STEP / 16);      // inner values of a token, 128 columns: two pieces and eight scales
@@ -52,6 +52,7 @@ constexpr uint32_t H_PITCH = H_BLOCK + 16;                        // the same in
 constexpr uint32_t MAX_DOWN_DEPTH = 8;
 constexpr uint64_t WAIT_LIMIT_CYCLES = 4000000000ull;
 constexpr uint32_t ALL = 0xffffffffu;
+constexpr uint32_t NEAR_ENTRIES = 64;     // entries that the second kernel has in shared memory
 
 // An entry of the list of chosen experts, as the second kernel needs it.
 struct Entry {
@@ -180,64 +181,85 @@ SQNN_DEV void weights_of(uint32_t (&a)[4], uint32_t top, uint32_t bottom)
 
 // ---- routing
 
+// Logits of this CTA's experts (every CLUSTER-th), as keys, into the shared memory of all CTAs of the cluster, and the tokens' largest
+// activations.  Waits for the cluster before it writes to others.  Some products at a time are summed in fp32, these sums in 64 bits: which experts a token goes to must not hang on the order of a sum.
+// `scratch`: 16 KB.
+// 64-bit floating numbers as integers of the same order; NaN comes last.  And back.
+SQNN_DEV int64_t key_of(double v)
+{
+    if (v != v) return 0x7fffffffffffffffll;
+    const int64_t b = __double_as_longlong(v == 0.0 ? 0.0 : v);
+    return b ^ ((b >> 63) & 0x7fffffffffffffffll);
+}
+SQNN_DEV double value_of(int64_t k) { return __longlong_as_double(k ^ ((k >> 63) & 0x7fffffffffffffffll)); }
+SQNN_DEV void send_logit(const MoeArgs &M, int64_t *keys, uint32_t token, uint32_t expert, double v)
+{
+    const uint32_t at = smem_addr(keys + token * M.experts + expert);
+    const int64_t key = key_of(v);
+#pragma unroll
+    for (uint32_t r = 0; r < CLUSTER; ++r) peer_store(peer_addr(at, r), key);
+}
+
+// 16 bf16 numbers of a row from `at` on, zero from `n` on.  (What is seldom run is kept out of line, here and below: the kernels run once
+// through most of their code, and fetching instructions is what that costs.)
+static __device__ __noinline__ uint4 ragged8(const __nv_bfloat16 *row, uint32_t at, uint32_t n)
+{
+    const uint16_t *const p = reinterpret_cast<const uint16_t *>(row);
+    uint32_t v[4];
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j)
+        v[j] = (at + 2 * j < n ? p[at + 2 * j] : 0u) | (at + 2 * j + 1 < n ? (uint32_t)p[at + 2 * j + 1] << 16 : 0u);
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+static __device__ __noinline__ float4 ragged4(const float *row, uint32_t at, uint32_t n)
+{
+    return make_float4(at < n ? row[at] : 0.0f, at + 1 < n ? row[at + 1] : 0.0f, at + 2 < n ? row[at + 2] : 0.0f, at + 3 < n ? row[at + 3] : 0.0f);
+}
+SQNN_DEV void raw16(const __nv_bfloat16 *row, uint32_t at, uint32_t n, bool vec, uint32_t (&v)[8])
+{
+    uint4 a, b;
+    if (vec && at + 16 <= n) {
+        a = *reinterpret_cast<const uint4 *>(row + at);
+        b = *reinterpret_cast<const uint4 *>(row + at + 8);
+    } else {
+        a = ragged8(row, at, n);
+        b = ragged8(row, at + 8, n);
+    }
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+
 SQNN_DEV void row_values8(const float *row, uint32_t at, uint32_t n, bool vec, float (&v)[8])
 {
+    float4 a, b;
     if (vec && at + 8 <= n) {
-        const float4 a = *reinterpret_cast<const float4 *>(row + at), b = *reinterpret_cast<const float4 *>(row + at + 4);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        a = *reinterpret_cast<const float4 *>(row + at);
+        b = *reinterpret_cast<const float4 *>(row + at + 4);
     } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) v[j] = at + j < n ? row[at + j] : 0.0f;
+        a = ragged4(row, at, n);
+        b = ragged4(row, at + 4, n);
     }
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
 SQNN_DEV void row_values8(const __nv_bfloat16 *row, uint32_t at, uint32_t n, bool vec, float (&v)[8])
 {
-    if (vec && at + 8 <= n) {
-        const uint4 f = *reinterpret_cast<const uint4 *>(row + at);
-        const uint32_t u[4] = {f.x, f.y, f.z, f.w};
+    const uint4 f = vec && at + 8 <= n ? *reinterpret_cast<const uint4 *>(row + at) : ragged8(row, at, n);
+    const uint32_t u[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(u[i] << 16);
-            v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) v[j] = at + j < n ? __bfloat162float(row[at + j]) : 0.0f;
-    }
-}
-
-// Logits of this CTA's experts (every CLUSTER-th) into the shared memory of all CTAs of the cluster, and the tokens' largest
-// activations.  Some products at a time are summed in fp32, these sums in 64 bits: which experts a token goes to must not hang on the order of a sum.
-// `scratch`: 16 KB.
-SQNN_DEV void send_logit(const MoeArgs &M, double *logits, uint32_t token, uint32_t expert, double v)
-{
-    const uint32_t at = smem_addr(logits + token * M.experts + expert);
-#pragma unroll 1
-    for (uint32_t r = 0; r < CLUSTER; ++r) peer_store(peer_addr(at, r), v);
-}
-
-// 16 bf16 numbers of a row from `at` on, zero from `n` on.
-SQNN_DEV void raw16(const __nv_bfloat16 *row, uint32_t at, uint32_t n, bool vec, uint32_t (&v)[8])
-{
-    if (vec && at + 16 <= n) {
-        const uint4 a = *reinterpret_cast<const uint4 *>(row + at), b = *reinterpret_cast<const uint4 *>(row + at + 8);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-        const uint16_t *const p = reinterpret_cast<const uint16_t *>(row);
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j)
-            v[j] = (at + 2 * j < n ? p[at + 2 * j] : 0u) | (at + 2 * j + 1 < n ? (uint32_t)p[at + 2 * j + 1] << 16 : 0u);
+    for (uint32_t i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(u[i] << 16);
+        v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
     }
 }
 
 // bf16: on the tensor cores, 16 experts by 8 tokens by 64 columns (four MMAs, products exact) at a time.  The columns of a tile are shared by as
 // many warps as there are to spare.
-SQNN_DEV void logits_of_cluster(const MoeArgs &M, double *logits, double *scratch, Routing &R, const __nv_bfloat16 *x, const __nv_bfloat16 *router)
+SQNN_DEV void logits_of_cluster(const MoeArgs &M, int64_t *keys, double *scratch, Routing &R, const __nv_bfloat16 *x, const __nv_bfloat16 *router)
 {
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3, rank = cluster_rank();
     // (a CTA without experts still looks at the tokens)
     const uint32_t mine = (M.experts - rank + CLUSTER - 1) / CLUSTER, n_tiles = (M.tokens + 7) / 8, tiles = (max(mine, 1u) + 15) / 16 * n_tiles;
     const uint32_t parts = tiles < WARPS ? WARPS / tiles : 1, steps = (M.hidden + 63) / 64;
+    if (parts == 1) cluster_wait();
 #pragma unroll 1
     for (uint32_t i = warp; i < tiles * parts; i += WARPS) {
         const uint32_t tile = i / parts, part = i - tile * parts, e0 = tile / n_tiles * 16, t0 = tile % n_tiles * 8;
@@ -274,27 +296,31 @@ SQNN_DEV void logits_of_cluster(const MoeArgs &M, double *logits, double *scratc
         for (uint32_t j = 0; j < 4; ++j) {
             const uint32_t e = e0 + g + (j >> 1) * 8, t = t0 + 2 * t4 + (j & 1);
             if (parts > 1) scratch[i * 128 + j * 32 + lane] = sum[j];
-            else if (e < mine && t < M.tokens) send_logit(M, logits, t, rank + CLUSTER * e, sum[j]);
+            else if (e < mine && t < M.tokens) send_logit(M, keys, t, rank + CLUSTER * e, sum[j]);
         }
     }
     if (parts == 1) return;
     __syncthreads();
+    cluster_wait();                                              // all CTAs of the cluster run: their shared memory may be written
 #pragma unroll 1
-    for (uint32_t i = tid; i < tiles * 128; i += THREADS) {
-        const uint32_t tile = i / 128, j = i / 32 & 3, l = i & 31, e = tile / n_tiles * 16 + (l >> 2) + (j >> 1) * 8, t = tile % n_tiles * 8 + 2 * (l & 3) + (j & 1);
+    for (uint32_t i4 = tid; i4 < tiles * 512; i4 += THREADS) {    // four threads per sum
+        const uint32_t i = i4 / 4, tile = i / 128, j = i / 32 & 3, l = i & 31, e = tile / n_tiles * 16 + (l >> 2) + (j >> 1) * 8, t = tile % n_tiles * 8 + 2 * (l & 3) + (j & 1);
         double sum = 0.0;
-        for (uint32_t p = 0; p < parts; ++p) sum += scratch[(tile * parts + p) * 128 + (i & 127)];
-        if (e < mine && t < M.tokens) send_logit(M, logits, t, rank + CLUSTER * e, sum);
+        for (uint32_t p = i4 & 3; p < parts; p += 4) sum += scratch[(tile * parts + p) * 128 + (i & 127)];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        if ((i4 & 3) == 0 && e < mine && t < M.tokens) send_logit(M, keys, t, rank + CLUSTER * e, sum);
     }
 }
 
 // fp32: a warp per expert, four tokens and a share of the columns; eight products at a time.
-SQNN_DEV void logits_of_cluster(const MoeArgs &M, double *logits, double *scratch, Routing &R, const float *x, const float *router)
+SQNN_DEV void logits_of_cluster(const MoeArgs &M, int64_t *keys, double *scratch, Routing &R, const float *x, const float *router)
 {
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank();
     constexpr uint32_t SHARE = 4;                                // tokens that share a read of an expert's row
     const uint32_t mine = (M.experts - rank + CLUSTER - 1) / CLUSTER, groups = (M.tokens + SHARE - 1) / SHARE, tasks = max(mine, 1u) * groups;
     const uint32_t parts = tasks < WARPS ? WARPS / tasks : 1, steps = (M.hidden + 255) / 256;
+    if (parts == 1) cluster_wait();
 #pragma unroll 1
     for (uint32_t i = warp; i < tasks * parts; i += WARPS) {
         const uint32_t task = i / parts, part = i - task * parts, own = task / groups, t0 = task % groups * SHARE;
@@ -326,60 +352,71 @@ SQNN_DEV void logits_of_cluster(const MoeArgs &M, double *logits, double *scratc
             if (lane == 0 && t0 + t < M.tokens) {
                 if (own == 0) atomicMax(&R.largest[t0 + t], most);
                 if (parts > 1) scratch[i * SHARE + t] = sum[t];
-                else if (own < mine) send_logit(M, logits, t0 + t, rank + CLUSTER * own, sum[t]);
+                else if (own < mine) send_logit(M, keys, t0 + t, rank + CLUSTER * own, sum[t]);
             }
         }
     }
     if (parts == 1) return;
     __syncthreads();
+    cluster_wait();
     if (tid < tasks * SHARE) {
         const uint32_t task = tid / SHARE, t = task % groups * SHARE + tid % SHARE;
         double sum = 0.0;
         for (uint32_t p = 0; p < parts; ++p) sum += scratch[(task * parts + p) * SHARE + tid % SHARE];
-        if (t < M.tokens && task / groups < mine) send_logit(M, logits, t, rank + CLUSTER * (task / groups), sum);
+        if (t < M.tokens && task / groups < mine) send_logit(M, keys, t, rank + CLUSTER * (task / groups), sum);
     }
 }
-
-// 64-bit floating numbers as integers of the same order; NaN comes last.  And back.
-SQNN_DEV int64_t key_of(double v)
-{
-    if (v != v) return 0x7fffffffffffffffll;
-    const int64_t b = __double_as_longlong(v == 0.0 ? 0.0 : v);
-    return b ^ ((b >> 63) & 0x7fffffffffffffffll);
-}
-SQNN_DEV double value_of(int64_t k) { return __longlong_as_double(k ^ ((k >> 63) & 0x7fffffffffffffffll)); }
 
 // From logits to the top_k experts of each token, their shares, and the list of (expert, group of up to `per` of its tokens), ascending.  NaN counts as the
-// largest, so that there are always top_k different experts.  All threads; begins and ends with a barrier.
-SQNN_DEV void choose(const MoeArgs &M, double *logits, Routing &R)
+// largest, so that there are always top_k different experts.  All threads; masks are zero before, ends with a barrier.  `chosen`: 8 KB.
+SQNN_DEV void choose(const MoeArgs &M, int64_t *keys, int64_t *chosen, Routing &R)
 {
-    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, all = M.tokens * M.experts, pairs = M.tokens * M.top_k;
-    int64_t *const keys = reinterpret_cast<int64_t *>(logits);
-    __syncthreads();
-    for (uint32_t i = tid; i < all; i += THREADS) keys[i] = key_of(logits[i]);
-    for (uint32_t i = tid; i < 2 * M.experts; i += THREADS) (&R.mask[0][0])[i] = 0;
-    __syncthreads();
-    // an expert's place is the number of those before it; four threads count
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // a warp per token: the largest key top_k times, by the upper half, the lower half, the index; the lane that has it notes it down
+    for (uint32_t t = warp; t < M.tokens; t += WARPS) {
+        int2 *const row = reinterpret_cast<int2 *>(keys + t * M.experts);
+        int2 *const best_of = reinterpret_cast<int2 *>(chosen + t * M.top_k);
+        int32_t *const ids = R.ids + t * M.top_k;
+        constexpr int32_t TAKEN = -0x7fffffff - 1;               // below all keys
 #pragma unroll 1
-    for (uint32_t i0 = 0; i0 < all; i0 += THREADS / 4) {
-        const uint32_t i = i0 + tid / 4, t = min(i, all - 1) / M.experts, e = min(i, all - 1) - t * M.experts;
-        const int64_t mine = keys[t * M.experts + e];
-        uint32_t place = 0;
-#pragma unroll 4
-        for (uint32_t j = tid & 3; j < M.experts; j += 4) place += keys[t * M.experts + j] > mine - (j < e ? 1 : 0) ? 1 : 0;
-        place += __shfl_xor_sync(0xffffffffu, place, 1);
-        place += __shfl_xor_sync(0xffffffffu, place, 2);
-        if (i < all && (tid & 3) == 0 && place < M.top_k) {
-            R.ids[t * M.top_k + place] = (int32_t)e;
-            atomicOr(&R.mask[e][t >> 5], 1u << (t & 31));
+        for (uint32_t s = 0; s < M.top_k; ++s) {
+            int2 best = make_int2(0, TAKEN);
+            uint32_t at = MAX_EXPERTS;
+            for (uint32_t e = lane; e < M.experts; e += 32) {
+                const int2 k = row[e];
+                if (k.y > best.y || (k.y == best.y && (uint32_t)k.x > (uint32_t)best.x)) { best = k; at = e; }
+            }
+            const int32_t upper = __reduce_max_sync(0xffffffffu, best.y);
+            bool mine = best.y == upper;
+            const uint32_t who = __ballot_sync(0xffffffffu, mine);
+            if (who & (who - 1)) {
+                const uint32_t lower = __reduce_max_sync(0xffffffffu, mine ? (uint32_t)best.x : 0u);
+                mine = mine && (uint32_t)best.x == lower;
+                const uint32_t lowest = __reduce_min_sync(0xffffffffu, mine ? at : MAX_EXPERTS);     // (by all lanes)
+                mine = mine && at == lowest;
+            }
+            if (mine) {
+                ids[s] = (int32_t)at;
+                best_of[s] = best;
+                row[at] = make_int2(0, TAKEN);
+            }
         }
+        __syncwarp();
+        const double first = value_of(chosen[t * M.top_k]);
+        float sum = 0.0f;
+        if (lane < M.top_k) {
+            sum = expf((float)(value_of(chosen[t * M.top_k + lane]) - first));
+            R.probs[t * M.top_k + lane] = sum;
+            atomicOr(&R.mask[ids[lane]][t >> 5], 1u << (t & 31));
+        }
+        if (!M.renormalize)
+            for (uint32_t e = lane; e < M.experts; e += 32)
+                if (row[e].y != TAKEN) sum += expf((float)(value_of(keys[t * M.experts + e]) - first));
+#pragma unroll
+        for (uint32_t d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0) R.total[t] = sum;
     }
     __syncthreads();
-    for (uint32_t i = tid; i < pairs; i += THREADS) {
-        const uint32_t t = i / M.top_k;
-        const int64_t *const k = keys + t * M.experts;
-        R.probs[i] = expf((float)(value_of(k[R.ids[i]]) - value_of(k[R.ids[t * M.top_k]])));
-    }
     static_assert(MAX_EXPERTS <= THREADS, "an expert per thread");
     const uint32_t groups = tid < M.experts ? (tokens_of(R, tid) + M.per - 1) / M.per : 0;
     uint32_t upto = groups;
@@ -390,23 +427,6 @@ SQNN_DEV void choose(const MoeArgs &M, double *logits, Routing &R)
     }
     if (lane == 31) R.totals[warp] = upto;
     __syncthreads();
-    if (M.renormalize) {
-        if (tid < M.tokens) {
-            float sum = 0.0f;
-            for (uint32_t s = 0; s < M.top_k; ++s) sum += R.probs[tid * M.top_k + s];
-            R.total[tid] = sum;
-        }
-    } else {
-        for (uint32_t t = warp; t < M.tokens; t += WARPS) {
-            const int64_t *const k = keys + t * M.experts;
-            const double first = value_of(k[R.ids[t * M.top_k]]);
-            float sum = 0.0f;
-            for (uint32_t e = lane; e < M.experts; e += 32) sum += expf((float)(value_of(k[e]) - first));
-#pragma unroll
-            for (uint32_t d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            if (lane == 0) R.total[t] = sum;
-        }
-    }
     uint32_t before = 0, count = 0;
 #pragma unroll
     for (uint32_t w = 0; w < WARPS; ++w) {
@@ -440,36 +460,41 @@ struct Walk {
     uint32_t window0, window1;    // the window's units
 };
 
-template <typename XT>
+// EARLY: there is room for all tokens of the call, so they are staged once, a row each, and there are no windows.
+template <typename XT, bool EARLY>
 __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ CUtensorMap weights, const MoeArgs M)
 {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     constexpr uint32_t PIECES = sizeof(XT) == 2 ? 1 : 2;
     __shared__ uint64_t bars[STREAMS * UP_DEPTH];
     __shared__ uint32_t abort_word;
-    // [rings][routing][partial sums][rows of x]; the logits, [tokens][experts], lie where the rings are later
+    // [rings][routing][partial sums of two rounds][rows of x]; the keys of the logits, [tokens][experts], lie where the rings are later
     const uint32_t skew = (1024u - (smem_addr(smem_raw) & 1023u)) & 1023u;
     uint8_t *const smem = smem_raw + skew;
-    static_assert(SQNN_MOE_MAX_LOGITS * sizeof(double) <= STREAMS * UP_DEPTH * UP_SLOT, "room for the logits");
+    static_assert(WARPS == 2 * STREAMS, "half of the warps stream, half join");
+    static_assert(SQNN_MOE_MAX_LOGITS * sizeof(int64_t) <= STREAMS * UP_DEPTH * UP_SLOT, "room for the logits");
     Routing &R = *reinterpret_cast<Routing *>(smem + STREAMS * UP_DEPTH * UP_SLOT);
-    double *const logits = reinterpret_cast<double *>(smem);
+    int64_t *const keys = reinterpret_cast<int64_t *>(smem);
     float *const parts = reinterpret_cast<float *>(smem + STREAMS * UP_DEPTH * UP_SLOT + ROUTING_BYTES);
-    uint8_t *const x_rows = reinterpret_cast<uint8_t *>(parts) + PARTS_BYTES;
+    uint8_t *const x_rows = reinterpret_cast<uint8_t *>(parts) + 2 * PARTS_BYTES;
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
     const Waits W{&abort_word, M.status, M.wait_limit};
     if (tid < STREAMS * UP_DEPTH) mbar_init(smem_addr(bars + tid), 1);
     if (tid == 0) abort_word = 0;
     if (tid < MAX_TOKENS) R.largest[tid] = 0;
+    for (uint32_t i = tid; i < 2 * M.experts; i += THREADS) (&R.mask[0][0])[i] = 0;
+    if (tid == 0) asm volatile("prefetch.tensormap [%0];\n" :: "l"(&weights) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     wait_prior_grid();
     launch_dependents();
-    cluster_sync();                                              // all CTAs of the cluster run: their shared memory may be written
-    logits_of_cluster(M, logits, reinterpret_cast<double *>(parts), R, static_cast<const XT *>(M.x), static_cast<const XT *>(M.router));
+    cluster_arrive();
+    logits_of_cluster(M, keys, reinterpret_cast<double *>(parts), R, static_cast<const XT *>(M.x), static_cast<const XT *>(M.router));
     cluster_sync();                                              // (the last time that one CTA writes to another)
     // Tokens, scaled and in fp16, to rows `base` and on: an expert's, from the first-th on, or all.
     const uint32_t steps = (M.hidden + STEP - 1) / STEP, lo_at = steps * STEP * 2;
     auto stage = [&](uint32_t base, uint32_t count, uint32_t expert, uint32_t first) {
         const uint32_t cols8 = steps * (STEP / 8);
+#pragma unroll 2
         for (uint32_t i = tid; i < count * cols8; i += THREADS) {
             const uint32_t k = i / cols8, at = (i - k * cols8) * 8, t = expert == ALL ? k : token_of(R, expert, first + k);
             const float s = scale_of(exponent_of(R.largest[t]));
@@ -492,11 +517,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
             }
         }
     };
-    const bool early = M.tokens <= M.x_rows;                     // there is room for all tokens: a row each, once and for all
-    if (early) stage(0, M.tokens, ALL, 0);
-    choose(M, logits, R);
-    fence_async_smem();                                          // the rings' copies come after what was read and written here
-    __syncthreads();
+    if constexpr (EARLY) stage(0, M.tokens, ALL, 0);
+    fence_async_smem();                                          // the rings' copies come after what was written there
+    choose(M, keys, reinterpret_cast<int64_t *>(parts), R);
     if (blockIdx.x == 0) {                                       // for the caller and for the second kernel
         for (uint32_t i = tid; i < M.tokens * M.top_k; i += THREADS) {
             if (M.ids_out) M.ids_out[i] = R.ids[i];
@@ -527,11 +550,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
         w.round0 = round0;
         w.left = 0;
         if (round0 >= u1) return;
-        if (round0 >= w.window1) {
+        if (EARLY) {
+            w.window0 = u0;
+            w.window1 = u1;
+        } else if (round0 >= w.window1) {
             uint32_t n = round0 / per_entry, rows = 0;
-            while (!early && n < R.entries && n * per_entry < u1 && rows + tokens_in(n) <= M.x_rows) rows += tokens_in(n++);
+            while (n < R.entries && n * per_entry < u1 && rows + tokens_in(n) <= M.x_rows) rows += tokens_in(n++);
             w.window0 = round0;
-            w.window1 = early ? u1 : min(u1, n * per_entry);
+            w.window1 = min(u1, n * per_entry);
         }
         w.round_n = min(STREAMS, w.window1 - round0);
         if (warp >= STREAMS) return;
@@ -550,6 +576,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
         const uint32_t n = ahead.u / per_entry;
         weight_row = (R.entry[n] & 0xffffu) * M.gu_expert + (ahead.u - n * per_entry) * 16;
     };
+    auto next_round = [&]() {                                    // to this warp's first step of the next round that has one
+#pragma unroll 1
+        do enter(ahead, ahead.round0 + ahead.round_n);
+        while (ahead.left == 0 && ahead.round0 < u1);
+        if (ahead.round0 < u1) open_unit();
+    };
     auto request = [&]() {
         if (ahead.round0 < u1) {
             if (lane == 0 && !M.skip_loads && !*W.abort_flag) {
@@ -559,27 +591,71 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
                 tma_load_2d(sa + UP_SLOT / 2, &weights, bar, (int32_t)(ahead.c * STEP), (int32_t)(weight_row + M.gu_half));
                 ++issued;
             }
-            bool same = true;
-            if (++ahead.c == steps) { ahead.c = 0; ++ahead.u; same = false; }
-            if (--ahead.left == 0) {
-                do enter(ahead, ahead.round0 + ahead.round_n);
-                while (ahead.left == 0 && ahead.round0 < u1);
-                same = false;
-            }
-            if (!same && ahead.round0 < u1) open_unit();
+            const bool over = ++ahead.c == steps;
+            if (over) { ahead.c = 0; ++ahead.u; }
+            if (--ahead.left == 0) next_round();
+            else if (over) open_unit();
             put_slot = put_slot + 1 == UP_DEPTH ? 0 : put_slot + 1;
         }
     };
     if (warp < STREAMS) {
-        enter(ahead, u0);
-        while (ahead.left == 0 && ahead.round0 < u1) enter(ahead, ahead.round0 + ahead.round_n);
-        if (ahead.round0 < u1) open_unit();
+        ahead.round0 = u0;
+        next_round();
 #pragma unroll 1
         for (uint32_t j = 0; j + 1 < UP_DEPTH; ++j) request();
     }
 
+    // A unit of a round that is over, by a warp of the second half: its parts in warp order, the gate, and out to h.  These warps work a round behind
+    // the others, which have gone on.
+    auto join = [&](uint32_t round0, uint32_t round_n, const float *from) {
+        const uint32_t k0 = warp - STREAMS;
+        if (__any_sync(0xffffffffu, k0 >= round_n || *W.abort_flag)) return;     // (all lanes or none)
+                    const uint32_t unit = round0 + k0, total = round_n * steps;
+                    float sum[8] = {};
+                    for (uint32_t q = 0; q < STREAMS; ++q) {
+                        const uint32_t a = total * q / STREAMS, b = total * (q + 1) / STREAMS;
+                        if (a >= b || b <= k0 * steps || a >= (k0 + 1) * steps) continue;
+                        const float *const p = from + ((q * 2 + (k0 - a / steps)) * 8) * 32 + lane;
+        #pragma unroll
+                        for (uint32_t j = 0; j < 8; ++j) sum[j] += p[j * 32];
+                    }
+                    const uint32_t n = unit / per_entry, en = R.entry[n], e = en & 0xffffu, q = unit - n * per_entry, count = tokens_in(n);
+                    const uint32_t i = q * 16 + g;                       // rows i and i + 8
+                    // where a row's value goes: 16 (row / 4 % 4) + 4 (q % 4) + row % 4 of its 64
+                    const uint32_t at = q / (STEP / 16) * H_BLOCK + ((q & 4) * 16 + (g >> 2) * 16 + (q & 3) * 4 + (g & 3)) * 2;
+        #pragma unroll
+                    for (uint32_t k = 0; k < 2; ++k) {
+                        const float a = sum[k], b = sum[2 + k];
+                        const float va = i < M.inner ? a / (1.0f + expf(-a)) * sum[4 + k] : 0.0f;
+                        const float vb = i + 8 < M.inner ? b / (1.0f + expf(-b)) * sum[6 + k] : 0.0f;
+                        uint32_t top = max(__float_as_uint(va) & 0x7fffffffu, __float_as_uint(vb) & 0x7fffffffu);
+        #pragma unroll
+                        for (uint32_t d = 4; d < 32; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+                        const uint32_t ex = exponent_of(top);
+                        const float s = scale_of(ex);
+                        const uint32_t hi = f16x2(va * s, vb * s), lo = f16x2(va * s - f16_lo(hi), vb * s - f16_hi(hi));
+                        const uint32_t column = 2 * t4 + k;
+                        if (column < count) {
+                            const uint32_t t = token_of(R, e, (en >> 16) * M.per + column);
+                            uint8_t *const row = M.h + (uint64_t)pair_of(R, M, t, e) * M.h_row;
+                            *reinterpret_cast<uint16_t *>(row + at) = (uint16_t)hi;
+                            *reinterpret_cast<uint16_t *>(row + at + 64) = (uint16_t)(hi >> 16);
+                            *reinterpret_cast<uint16_t *>(row + at + 256) = (uint16_t)lo;
+                            *reinterpret_cast<uint16_t *>(row + at + 320) = (uint16_t)(lo >> 16);
+                            if (g == 0) *reinterpret_cast<float *>(row + q / 8 * H_BLOCK + 512 + (q & 7) * 4) = back_of(ex);
+                            if (q + 1 == per_entry)                      // the rest of the last block is zero
+                                for (uint32_t z = q + 1; z & 7; ++z) {
+                                    const uint32_t to = z / 8 * H_BLOCK + ((z & 4) * 16 + (g >> 2) * 16 + (z & 3) * 4 + (g & 3)) * 2;
+                                    *reinterpret_cast<uint16_t *>(row + to) = *reinterpret_cast<uint16_t *>(row + to + 64) = 0;
+                                    *reinterpret_cast<uint16_t *>(row + to + 256) = *reinterpret_cast<uint16_t *>(row + to + 320) = 0;
+                                    if (g == 0) *reinterpret_cast<float *>(row + z / 8 * H_BLOCK + 512 + (z & 7) * 4) = 0.0f;
+                                }
+                        }
+                    }
+    };
     Walk w;
     w.window1 = w.round_n = 0;
+    uint32_t done0 = 0, done_n = 0, parity = 0;                  // the round before
     uint32_t get_slot = 0, get_parity = 0;
     const uint32_t row_at = matrix_row(lane);
     const float *unit_scale = nullptr;                           // the unit's scales of G; those of U `to_up` further on
@@ -599,7 +675,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
         const bool fresh = round0 >= w.window1;
         enter(w, round0);
         if (w.left) scales_of_unit();
-        if (fresh && !early) {                                   // the window's tokens
+        if (!EARLY && fresh) {                                   // the window's tokens
             const uint32_t n1 = (w.window1 + per_entry - 1) / per_entry;
             uint32_t base = 0;
             for (uint32_t n = w.window0 / per_entry; n < n1; ++n) {
@@ -609,16 +685,18 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
             }
             __syncthreads();
         }
-        // ---- this warp's steps of the round
-        if (warp < STREAMS) {
+        // ---- the second half joins the round before, the first half takes its steps of this one
+        if (warp >= STREAMS) {
+            if (done_n) join(done0, done_n, parts + (parity ^ 1) * (PARTS_BYTES / 4));
+        } else {
             const uint32_t first_unit = w.u;
             float acc[8] = {};
             uint32_t x_at = 0;
             float b0 = 0.0f, b1 = 0.0f;
             auto begin = [&]() {                                 // where the tokens of the unit's entry are, and their scales
                 const uint32_t n0 = w.window0 / per_entry, n = w.u / per_entry, en = R.entry[n], e = en & 0xffffu, first = (en >> 16) * M.per, count = tokens_in(n);
-                uint32_t row = early ? token_of(R, e, first + min(g, count - 1)) : min(g, count - 1);
-                for (uint32_t k = n0; k < n && !early; ++k) row += tokens_in(k);
+                uint32_t row = EARLY ? token_of(R, e, first + min(g, count - 1)) : min(g, count - 1);
+                for (uint32_t k = n0; !EARLY && k < n; ++k) row += tokens_in(k);
                 x_at = smem_addr(x_rows) + row * M.x_row + t4 * 32;                          // columns without a token repeat the last one; nobody looks at them
                 b0 = back_of(exponent_of(R.largest[token_of(R, e, first + min(2 * t4, count - 1))]));
                 b1 = back_of(exponent_of(R.largest[token_of(R, e, first + min(2 * t4 + 1, count - 1))]));
@@ -667,7 +745,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
                     acc[4 + j] = fmaf(cu[0][j] + cu[1][j], su * (j & 1 ? b1 : b0), acc[4 + j]);
                 }
                 if (end) {
-                    float *const p = parts + ((warp * 2 + (unit - first_unit)) * 8) * 32 + lane;
+                    float *const p = parts + parity * (PARTS_BYTES / 4) + ((warp * 2 + (unit - first_unit)) * 8) * 32 + lane;
 #pragma unroll
                     for (uint32_t j = 0; j < 8; ++j) { p[j * 32] = acc[j]; acc[j] = 0.0f; }
                     if (w.left) begin();
@@ -675,53 +753,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
             }
         }
         __syncthreads();
-        // ---- a warp per unit: its parts in warp order, the gate, and out to h
-        if (warp < w.round_n && !*W.abort_flag) {
-            const uint32_t unit = round0 + warp, total = w.round_n * steps;
-            float sum[8] = {};
-            for (uint32_t q = 0; q < STREAMS; ++q) {
-                const uint32_t a = total * q / STREAMS, b = total * (q + 1) / STREAMS;
-                if (a >= b || b <= warp * steps || a >= (warp + 1) * steps) continue;
-                const float *const p = parts + ((q * 2 + (warp - a / steps)) * 8) * 32 + lane;
-#pragma unroll
-                for (uint32_t j = 0; j < 8; ++j) sum[j] += p[j * 32];
-            }
-            const uint32_t n = unit / per_entry, en = R.entry[n], e = en & 0xffffu, q = unit - n * per_entry, count = tokens_in(n);
-            const uint32_t i = q * 16 + g;                       // rows i and i + 8
-            // where a row's value goes: 16 (row / 4 % 4) + 4 (q % 4) + row % 4 of its 64
-            const uint32_t at = q / (STEP / 16) * H_BLOCK + ((q & 4) * 16 + (g >> 2) * 16 + (q & 3) * 4 + (g & 3)) * 2;
-#pragma unroll
-            for (uint32_t k = 0; k < 2; ++k) {
-                const float a = sum[k], b = sum[2 + k];
-                const float va = i < M.inner ? a / (1.0f + expf(-a)) * sum[4 + k] : 0.0f;
-                const float vb = i + 8 < M.inner ? b / (1.0f + expf(-b)) * sum[6 + k] : 0.0f;
-                uint32_t top = max(__float_as_uint(va) & 0x7fffffffu, __float_as_uint(vb) & 0x7fffffffu);
-#pragma unroll
-                for (uint32_t d = 4; d < 32; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-                const uint32_t ex = exponent_of(top);
-                const float s = scale_of(ex);
-                const uint32_t hi = f16x2(va * s, vb * s), lo = f16x2(va * s - f16_lo(hi), vb * s - f16_hi(hi));
-                const uint32_t column = 2 * t4 + k;
-                if (column < count) {
-                    const uint32_t t = token_of(R, e, (en >> 16) * M.per + column);
-                    uint8_t *const row = M.h + (uint64_t)pair_of(R, M, t, e) * M.h_row;
-                    *reinterpret_cast<uint16_t *>(row + at) = (uint16_t)hi;
-                    *reinterpret_cast<uint16_t *>(row + at + 64) = (uint16_t)(hi >> 16);
-                    *reinterpret_cast<uint16_t *>(row + at + 256) = (uint16_t)lo;
-                    *reinterpret_cast<uint16_t *>(row + at + 320) = (uint16_t)(lo >> 16);
-                    if (g == 0) *reinterpret_cast<float *>(row + q / 8 * H_BLOCK + 512 + (q & 7) * 4) = back_of(ex);
-                    if (q + 1 == per_entry)                      // the rest of the last block is zero
-                        for (uint32_t z = q + 1; z & 7; ++z) {
-                            const uint32_t to = z / 8 * H_BLOCK + ((z & 4) * 16 + (g >> 2) * 16 + (z & 3) * 4 + (g & 3)) * 2;
-                            *reinterpret_cast<uint16_t *>(row + to) = *reinterpret_cast<uint16_t *>(row + to + 64) = 0;
-                            *reinterpret_cast<uint16_t *>(row + to + 256) = *reinterpret_cast<uint16_t *>(row + to + 320) = 0;
-                            if (g == 0) *reinterpret_cast<float *>(row + z / 8 * H_BLOCK + 512 + (z & 7) * 4) = 0.0f;
-                        }
-                }
-            }
-        }
-        __syncthreads();
+        done0 = round0;
+        done_n = w.round_n;
+        parity ^= 1;
     }
+    if (warp >= STREAMS && done_n) join(done0, done_n, parts + (parity ^ 1) * (PARTS_BYTES / 4));
+    __syncthreads();
     // after a wait that gave up: copies in flight must land before the block's shared memory goes away
     if (warp < STREAMS && lane == 0 && *W.abort_flag)
         for (uint32_t s = 0; s < UP_DEPTH; ++s) {
@@ -738,7 +775,8 @@ __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_co
     constexpr uint32_t TILES = ROWS / 16, W_BYTES = ROWS * STEP;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ uint64_t bars[DOWN_WARPS * MAX_DOWN_DEPTH];
-    __shared__ uint32_t abort_word;
+    __shared__ Entry near[NEAR_ENTRIES];
+    __shared__ uint32_t abort_word, list_size;
     // [ring of weights][ring of inner values][sums: warp, token, row]
     const uint32_t skew = (1024u - (smem_addr(smem_raw) & 1023u)) & 1023u, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
     uint8_t *const smem = smem_raw + skew;
@@ -751,12 +789,19 @@ __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_co
     for (uint32_t i = lane; i < M.tokens * ROWS; i += 32) mine[i] = 0.0f;
     if (lane < M.depth) mbar_init(my_bars + 8 * lane, 1);
     if (tid == 0) abort_word = 0;
+    if (tid == 0) asm volatile("prefetch.tensormap [%0];\n" :: "l"(&weights) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     __syncthreads();
     wait_prior_grid();
     launch_dependents();
     asm volatile("fence.proxy.async.global;\n" ::: "memory");    // the copies below read what the first kernel stored
-    const uint32_t steps = (M.inner + STEP - 1) / STEP, total = *M.list_size * steps;
+    // the list is read before its length is known, as far as it may reach: one trip to memory
+    for (uint32_t i = tid; i < min(M.tokens * M.top_k, NEAR_ENTRIES) * (uint32_t)(sizeof(Entry) / 4); i += DOWN_WARPS * 32)
+        reinterpret_cast<uint32_t *>(near)[i] = reinterpret_cast<const uint32_t *>(M.list)[i];
+    if (tid == 0) list_size = *M.list_size;
+    __syncthreads();
+    auto entry = [&](uint32_t n) -> const Entry & { return n < NEAR_ENTRIES ? near[n] : M.list[n]; };
+    const uint32_t steps = (M.inner + STEP - 1) / STEP, total = list_size * steps;
     const uint32_t q0 = total * warp / DOWN_WARPS, q1 = total * (warp + 1) / DOWN_WARPS;
 
     // ---- a step's weights and its tokens' inner values into the rings
@@ -764,7 +809,7 @@ __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_co
     uint32_t weight_row = 0, ahead_count = 0;
     const uint8_t *h_row = nullptr;                              // of token `lane`
     auto open_entry = [&]() {
-        const Entry &E = M.list[ahead_n];
+        const Entry &E = entry(ahead_n);
         ahead_count = E.count;
         weight_row = E.expert * M.d_expert + row0;
         h_row = M.h + (uint64_t)E.pair[lane < ahead_count ? lane : 0] * M.h_row;
@@ -803,13 +848,13 @@ __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_co
     auto scales_of = [&](uint32_t expert) { return M.down_scale + ((uint64_t)expert * ((M.hidden + FP8_BLOCK - 1) / FP8_BLOCK) + row0 / FP8_BLOCK) * steps; };
     auto look_ahead = [&]() {
         if ((uint64_t)(n + 1) * steps < q1) {
-            next_expert = M.list[n + 1].expert;
-            next_count = M.list[n + 1].count;
+            next_expert = entry(n + 1).expert;
+            next_count = entry(n + 1).count;
         }
     };
     if (q0 < q1) {
-        count = M.list[n].count;
-        entry_scale = scales_of(M.list[n].expert);
+        count = entry(n).count;
+        entry_scale = scales_of(entry(n).expert);
         next_s = ldg_ahead(reinterpret_cast<const uint32_t *>(entry_scale + c_at));
         look_ahead();
     }
@@ -852,7 +897,7 @@ __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_co
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) acc[r][j] = fmaf(part[r][j], s, acc[r][j]);
         if (++c_at == steps || q + 1 == q1) {                    // the entry's part goes to the warp's sums
-            const Entry &E = M.list[n];
+            const Entry &E = entry(n);
 #pragma unroll
             for (uint32_t k = 0; k < 2; ++k)
                 if (2 * t4 + k < count) {
@@ -924,19 +969,19 @@ bool make_map(CUtensorMap *map, const void *p, uint32_t n, uint64_t rows, int64_
 template <typename XT>
 int launch_moe(MoeArgs M, const sqnn_moe *L, cudaStream_t st)
 {
-    auto up = k_moe_up<XT>;
     // first kernel: what the ring and the partial sums leave holds rows of x
     const uint32_t cols = (M.hidden + STEP - 1) / STEP * STEP, pieces = sizeof(XT) == 2 ? 1 : 2;
-    const size_t fixed = 1024 + STREAMS * UP_DEPTH * UP_SLOT + ROUTING_BYTES + PARTS_BYTES;
+    const size_t fixed = 1024 + STREAMS * UP_DEPTH * UP_SLOT + ROUTING_BYTES + 2 * PARTS_BYTES;
     M.x_row = cols * 2 * pieces + 16;                            // 16 bytes past a multiple of 128: neighbouring rows in neighbouring banks
     M.x_rows = (uint32_t)((SMEM_BYTES - fixed) / M.x_row);
     if (M.x_rows == 0) return SQNN_E_UNSUPPORTED;
     M.per = M.x_rows < GROUP ? M.x_rows : GROUP;
+    auto up = M.tokens <= M.x_rows ? k_moe_up<XT, true> : k_moe_up<XT, false>;
     // second kernel: 32 rows per CTA where that still makes two CTAs for three SMs; as deep a ring as there is room for
     const uint32_t rows = 3 * ((M.hidden + 31) / 32) >= 2 * (uint32_t)sm_count() ? 32 : 16;
     M.slot = rows * STEP + (M.tokens < M.per ? M.tokens : M.per) * H_PITCH;
     const size_t sums = (size_t)DOWN_WARPS * M.tokens * rows * 4;
-    M.depth = (uint32_t)((SMEM_BYTES - 1024 - sums) / (DOWN_WARPS * M.slot));
+    M.depth = (uint32_t)((DOWN_SMEM_BYTES - 1024 - sums) / (DOWN_WARPS * M.slot));
     M.depth = M.depth < MAX_DOWN_DEPTH ? M.depth : MAX_DOWN_DEPTH;
     const size_t smem_down = 1024 + sums + (size_t)DOWN_WARPS * M.depth * M.slot;
     CUtensorMap gu_map, d_map;

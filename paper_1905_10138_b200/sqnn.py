@@ -20,7 +20,7 @@ LIB_PATH = os.environ.get("SQNN_LIBRARY") or os.path.join(_HERE, "libsqnn.so")
 
 MAX_PLANES = 8
 FP8_BLOCK = 128
-MOE_MAX_TOKENS, MOE_MAX_EXPERTS, MOE_MAX_TOP_K, MOE_MAX_LOGITS, MOE_MAX_WIDTH = 64, 512, 16, 16384, 14336
+MOE_MAX_TOKENS, MOE_MAX_EXPERTS, MOE_MAX_TOP_K, MOE_MAX_LOGITS, MOE_MAX_WIDTH = 64, 512, 16, 16384, 11264
 STATIC_SCRATCH_BYTES = 8 << 20
 OUT_BITS, OUT_BF16, OUT_SINK = 0, 1, 2
 X_F32, X_BF16 = 0, 1
