@@ -572,6 +572,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
     Walk ahead;
     ahead.window1 = ahead.round_n = 0;
     uint32_t weight_row = 0, put_slot = 0, issued = 0;
+    const uint64_t once = policy_once();
     auto open_unit = [&]() {
         const uint32_t n = ahead.u / per_entry;
         weight_row = (R.entry[n] & 0xffffu) * M.gu_expert + (ahead.u - n * per_entry) * 16;
@@ -587,8 +588,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
             if (lane == 0 && !M.skip_loads && !*W.abort_flag) {
                 const uint32_t bar = my_bars + 8 * put_slot, sa = ring + put_slot * UP_SLOT;
                 mbar_expect_tx(bar, UP_SLOT);
-                tma_load_2d(sa, &weights, bar, (int32_t)(ahead.c * STEP), (int32_t)weight_row);
-                tma_load_2d(sa + UP_SLOT / 2, &weights, bar, (int32_t)(ahead.c * STEP), (int32_t)(weight_row + M.gu_half));
+                tma_load_2d_once(sa, &weights, bar, (int32_t)(ahead.c * STEP), (int32_t)weight_row, once);
+                tma_load_2d_once(sa + UP_SLOT / 2, &weights, bar, (int32_t)(ahead.c * STEP), (int32_t)(weight_row + M.gu_half), once);
                 ++issued;
             }
             const bool over = ++ahead.c == steps;
@@ -807,6 +808,7 @@ __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_co
     // ---- a step's weights and its tokens' inner values into the rings
     uint32_t ahead_n = q0 / steps, ahead_c = q0 - ahead_n * steps, ahead_q = q0, put_slot = 0, issued = 0;
     uint32_t weight_row = 0, ahead_count = 0;
+    const uint64_t once = policy_once();
     const uint8_t *h_row = nullptr;                              // of token `lane`
     auto open_entry = [&]() {
         const Entry &E = entry(ahead_n);
@@ -820,7 +822,7 @@ __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_co
             const bool go = !M.skip_loads && !*W.abort_flag;
             if (lane == 0 && go) {
                 mbar_expect_tx(bar, W_BYTES + ahead_count * H_BLOCK);
-                tma_load_2d(ring + put_slot * W_BYTES, &weights, bar, (int32_t)(ahead_c * STEP), (int32_t)weight_row);
+                tma_load_2d_once(ring + put_slot * W_BYTES, &weights, bar, (int32_t)(ahead_c * STEP), (int32_t)weight_row, once);
                 ++issued;
             }
             const bool all_go = __shfl_sync(0xffffffffu, (int)go, 0) != 0;

@@ -73,6 +73,18 @@ SQNN_DEV void tma_load_2d(uint32_t sdst, const CUtensorMap *map, uint32_t bar, i
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n"
                  :: "r"(sdst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
 }
+// The same for what is read once: it leaves L2 before anything else does.
+SQNN_DEV uint64_t policy_once()
+{
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;\n" : "=l"(p));
+    return p;
+}
+SQNN_DEV void tma_load_2d_once(uint32_t sdst, const CUtensorMap *map, uint32_t bar, int32_t x, int32_t y, uint64_t policy)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4}], [%2], %5;\n"
+                 :: "r"(sdst), "l"(map), "r"(bar), "r"(x), "r"(y), "l"(policy) : "memory");
+}
 SQNN_DEV void tmem_alloc(uint32_t *slot, uint32_t cols)
 {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n"
