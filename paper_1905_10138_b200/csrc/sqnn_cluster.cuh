@@ -31,6 +31,20 @@ SQNN_DEV uint32_t peer_load(uint32_t a)
     return v;
 }
 
+SQNN_DEV void peer_store(uint32_t a, float v)
+{
+    asm volatile("st.shared::cluster.f32 [%0], %1;\n" :: "r"(a), "f"(v) : "memory");
+}
+SQNN_DEV void peer_store4(uint32_t a, float4 v)
+{
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};\n" :: "r"(a), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+// On a barrier of another block (an address of peer_addr).  Orders nothing but this thread's tensor-memory loads, which it has waited for and fenced: a
+// release over the cluster took over a thousand cycles.
+SQNN_DEV void peer_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];\n" :: "r"(bar) : "memory");
+}
 SQNN_DEV void peer_store(uint32_t a, int64_t v)
 {
     asm volatile("st.shared::cluster.s64 [%0], %1;\n" :: "r"(a), "l"(v) : "memory");

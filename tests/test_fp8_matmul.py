@@ -66,6 +66,14 @@ def test_larger(m, n, batch, y_type):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("m,n,batch", [(4099, 300, 1500), (1030, 4000, 1025), (700, 900, 129), (1500, 2000, 4200)])
+@pytest.mark.parametrize("y_type", [F32, BF16])
+@pytest.mark.parametrize("pad", [0, 1, 2, 4])
+def test_rows_of_y_on_and_off_boundaries(m, n, batch, y_type, pad):
+    run(m, n, batch, y_type, pad)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("batch", [3, 40, 200])
 def test_strides(batch):
     ops = operands(260, 900, batch, 4)
@@ -80,7 +88,7 @@ def test_strides(batch):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("batch", [1, 48, 130, 300])
+@pytest.mark.parametrize("batch", [1, 48, 130, 300, 4000])
 def test_results_are_the_same_from_run_to_run(batch):
     ops = operands(1030, 5000, batch, 5)
     first = product(*ops)
@@ -140,7 +148,7 @@ def test_own_stream_graph_and_two_at_once():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("m,n,batch", [(300, 4000, 7), (300, 4000, 90), (4096, 300, 2000)])
+@pytest.mark.parametrize("m,n,batch", [(300, 4000, 7), (300, 4000, 90), (4096, 300, 2000), (4096, 4000, 500)])
 def test_a_wait_that_gives_up_ends_the_call(m, n, batch):
     ops = operands(m, n, batch, 11)
     good = product(*ops)
