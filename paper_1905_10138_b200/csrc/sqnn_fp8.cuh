@@ -15,15 +15,4 @@ SQNN_DEV uint32_t to_fp8x2(float lo, float hi)
     return v;
 }
 
-// Whether an fp32 number within 448 lies within six of its last places of the middle between two neighbouring e4m3 numbers.  Above
-// 2^-6 a middle is where the 20 bits behind the three kept are 1000...; below, where e4m3 numbers are 2^-9 apart, 2^-6 is
-// added first: that puts the number where the spacing is the same.
-SQNN_DEV bool near_fp8_border(float t)
-{
-    float a = fabsf(t);
-    a = a < 0x1p-6f ? a + 0x1p-6f : a;
-    const uint32_t behind = __float_as_uint(a) & 0xfffffu;
-    return behind - (0x80000u - 6u) <= 12u;
-}
-
 }  // namespace sqnn

@@ -9,7 +9,7 @@
 // of mma.sync m16n8k16 with up to eight tokens as the columns of B.  (mma.sync, not tcgen05: weights that are used once gain nothing
 // from a tile that many warps share, and the rate of mma.sync is several times what memory asks for.  Weights read straight into registers, 62 us
 // for one token and 8 of 64 experts of 2048 x 1024: the unrolled code did not fit the instruction cache.  A ring filled by 16-byte copies of
-// every lane, 38 us: 230 to 280 instructions per kilobyte or two, most of them addresses.  This form: @T1@.)
+// every lane, 38 us: 230 to 280 instructions per kilobyte or two, most of them addresses.  This form: 26 us.)
 // The 16 columns of an MMA are dealt so that its k slots 2 t, 2 t + 1, 2 t + 8, 2 t + 9 are columns 4 t .. 4 t + 3, and B is stored
 // in the order that gives a lane its share of four MMAs in 32 bytes: position 16 t + 4 j + i of 64 holds column 16 j + 4 t + i.
 //

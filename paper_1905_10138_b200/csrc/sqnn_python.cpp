@@ -24,11 +24,12 @@ decltype(&sqnn_rmsnorm_fp8) f_rmsnorm_fp8 = nullptr;
 decltype(&sqnn_fp8_matmul) f_fp8_matmul = nullptr;
 decltype(&sqnn_moe_fp8) f_moe_fp8 = nullptr;
 
+// The three functions of encrypted layers, and up to three of 8-bit ones (a function without an address cannot be called).
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    if (nargs != 6) { PyErr_SetString(PyExc_TypeError, "bind takes six addresses"); return nullptr; }
-    void *p[6];
-    for (int i = 0; i < 6; ++i) {
+    if (nargs < 3 || nargs > 6) { PyErr_SetString(PyExc_TypeError, "bind takes three to six addresses"); return nullptr; }
+    void *p[6] = {};
+    for (Py_ssize_t i = 0; i < nargs; ++i) {
         p[i] = PyLong_AsVoidPtr(args[i]);
         if (PyErr_Occurred()) return nullptr;
     }
@@ -228,6 +229,13 @@ bool fail(const char *what)
     PyErr_SetString(PyExc_ValueError, what);
     return false;
 }
+template <typename F>
+bool bound(F f)
+{
+    if (f) return true;
+    PyErr_SetString(PyExc_RuntimeError, "this function was not bound");
+    return false;
+}
 bool on_device(const at::Tensor *t, const char *name)
 {
     if (!t) return true;
@@ -268,7 +276,7 @@ constexpr int64_t blocks_of(int64_t n) { return (n + SQNN_FP8_BLOCK - 1) / SQNN_
 PyObject *rmsnorm_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs)
 {
     return guarded([&]() -> PyObject * {
-        if (!enough(nargs, 9)) return nullptr;
+        if (!bound(f_rmsnorm_fp8) || !enough(nargs, 9)) return nullptr;
         const at::Tensor *x, *w, *q, *scale, *r, *h, *y;
         void *st;
         if (!tensor_arg(a[0], &x) || !tensor_arg(a[1], &w) || !tensor_arg(a[3], &q) || !tensor_arg(a[4], &scale) ||
@@ -319,7 +327,7 @@ bool status_word(const at::Tensor *t)
 PyObject *fp8_matmul(PyObject *, PyObject *const *a, Py_ssize_t nargs)
 {
     return guarded([&]() -> PyObject * {
-        if (!enough(nargs, 7)) return nullptr;
+        if (!bound(f_fp8_matmul) || !enough(nargs, 7)) return nullptr;
         const at::Tensor *w, *ws, *x, *xs, *y, *status;
         void *st;
         if (!tensor_arg(a[0], &w) || !tensor_arg(a[1], &ws) || !tensor_arg(a[2], &x) || !tensor_arg(a[3], &xs) || !tensor_arg(a[4], &y) ||
@@ -355,7 +363,7 @@ PyObject *fp8_matmul(PyObject *, PyObject *const *a, Py_ssize_t nargs)
 PyObject *moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs)
 {
     return guarded([&]() -> PyObject * {
-        if (!enough(nargs, 14)) return nullptr;
+        if (!bound(f_moe_fp8) || !enough(nargs, 14)) return nullptr;
         const at::Tensor *x, *router, *gu, *gus, *down, *downs, *y, *ws, *ids, *probs, *status;
         void *st;
         if (!tensor_arg(a[12], &status) || !tensor_arg(a[0], &x) || !tensor_arg(a[1], &router) || !tensor_arg(a[4], &gu) || !tensor_arg(a[5], &gus) || !tensor_arg(a[6], &down) ||
