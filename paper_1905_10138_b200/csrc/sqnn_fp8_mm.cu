@@ -63,8 +63,8 @@ SQNN_DEV void mma_block(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_
                  " add.u64 a1, %1, 2;\n add.u64 a2, %1, 4;\n add.u64 a3, %1, 6;\n"
                  " add.u64 b1, %2, 2;\n add.u64 b2, %2, 4;\n add.u64 b3, %2, 6;\n"
                  SQNN_MMA("%1", "%2", "f") SQNN_MMA("a1", "b1", "t") SQNN_MMA("a2", "b2", "t") SQNN_MMA("a3", "b3", "t")
-                 " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n"
-                 " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n}\n"
+                 " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n"
+                 " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n}\n"
                  :: "r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(free_stage), "r"(acc_full) : "memory");
 #undef SQNN_MMA
 }
@@ -77,8 +77,8 @@ SQNN_DEV void mma_block_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, ui
                  " add.u64 a1, %1, 2;\n add.u64 a2, %1, 4;\n add.u64 a3, %1, 6;\n"
                  " add.u64 b1, %2, 2;\n add.u64 b2, %2, 4;\n add.u64 b3, %2, 6;\n"
                  SQNN_MMA("%1", "%2", "f") SQNN_MMA("a1", "b1", "t") SQNN_MMA("a2", "b2", "t") SQNN_MMA("a3", "b3", "t")
-                 " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%4], m;\n"
-                 " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], m;\n}\n"
+                 " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], m;\n"
+                 " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%4], m;\n}\n"
                  :: "r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(free_stage), "r"(acc_full), "r"(mask) : "memory");
 #undef SQNN_MMA
 }
@@ -445,8 +445,8 @@ k_fp8_mm(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ C
         uint32_t stage = 0, parity = 0, it = 0;
         for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
             const uint32_t buf = it % BUFS, use = it / BUFS;
-            if (use > 0 && !mbar_wait_warp(acc_empty + 8 * buf, (use - 1) & 1u, abort_flag, M.status, M.wait_limit)) goto leave;
             if (!mbar_wait_warp(full + 8 * stage, parity, abort_flag, M.status, M.wait_limit)) goto leave;
+            if (use > 0 && !mbar_wait_warp(acc_empty + 8 * buf, (use - 1) & 1u, abort_flag, M.status, M.wait_limit)) goto leave;
             tc_fence_after();
             const uint64_t a = desc0 + stage * (STAGE >> 4);
             mma_block(tmem_base + buf * N, a, a + (A_BYTES >> 4), idesc, empty + 8 * stage, acc_full + 8 * buf);
@@ -584,8 +584,8 @@ k_fp8_mm_pair(const __grid_constant__ CUtensorMap x_map, const __grid_constant__
         for (uint32_t tile = first_tile; tile < M.tiles; tile += tile_step) {
             for (uint32_t k = k_begin; k < k_end; ++k, ++it) {
                 const uint32_t buf = it % BUFS, use = it / BUFS;
-                if (use > 0 && !mbar_wait_warp(acc_empty + 8 * buf, (use - 1) & 1u, abort_flag, M.status, M.wait_limit)) goto leave;
                 if (!mbar_wait_warp(full + 8 * stage, parity, abort_flag, M.status, M.wait_limit)) goto leave;
+                if (use > 0 && !mbar_wait_warp(acc_empty + 8 * buf, (use - 1) & 1u, abort_flag, M.status, M.wait_limit)) goto leave;
                 tc_fence_after();
                 const uint64_t a = desc0 + stage * (PAIR_STAGE >> 4);
                 mma_block_pair(tmem_base + buf * N, a, a + (PAIR_STAGE / 2 >> 4), idesc, empty + 8 * stage, acc_full + 8 * buf, mask);
