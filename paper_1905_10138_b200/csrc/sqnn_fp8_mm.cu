@@ -23,9 +23,7 @@
 
 #include <cuda_bf16.h>
 
-#include <map>
-#include <mutex>
-#include <tuple>
+#include <atomic>
 
 namespace sqnn {
 
@@ -48,7 +46,6 @@ struct Fp8Args {
     uint32_t stages;
     uint32_t y_bf16, vec, vec4;   // rows of Y on 16-byte boundaries; on those of four elements
     uint32_t xs_vec;              // rows of the activations' scales on 16-byte boundaries
-    uint32_t prefetch;            // weights are asked into L2 before the kernel before is over
     uint32_t skip_loads;          // test only: the loader issues no loads
     uint64_t wait_limit;
     uint32_t *status;
@@ -354,9 +351,6 @@ k_fp8_mm(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ C
             mbar_init(chunk_bar, PW);
             mbar_init(over, 1);
             abort_word = 0;
-            // the first weights on their way into L2 while the kernel before finishes
-            for (uint32_t k = k_begin; k < min(k_end, k_begin + M.stages) && M.prefetch; ++k)
-                tma_prefetch_2d(SWAP ? &lane_map : &col_map, (int32_t)(k * KB), (int32_t)(SWAP ? tl * LANES : tc * N));
         }
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
@@ -659,16 +653,14 @@ struct Operands {
     uint64_t n;
 };
 
-// How many clusters of this size run at once (asked for once per kernel, size and device).
-uint32_t clusters_at_once(const void *kernel, uint32_t cluster, uint32_t threads, size_t smem)
-{
-    static std::mutex mu;
-    static std::map<std::tuple<const void *, uint32_t, size_t, int>, uint32_t> known;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || ensure_dynamic_smem(kernel, smem) != SQNN_OK) return 0;
-    std::lock_guard<std::mutex> lock(mu);
-    uint32_t &have = known[std::make_tuple(kernel, cluster, smem, dev)];
-    if (!have) {
+// How many clusters of each size run at once: asked for once per kernel and device.  (A table and no lock: a small product's kernel takes 3 us.)
+struct AtOnce {
+    std::atomic<uint32_t> known[64][9];
+    uint32_t operator()(int dev, const void *kernel, uint32_t cluster, uint32_t threads, size_t smem)
+    {
+        uint32_t n = known[dev][cluster].load(std::memory_order_relaxed);
+        if (n) return n;
+        if (ensure_dynamic_smem(kernel, smem) != SQNN_OK) return 0;
         cudaLaunchAttribute attr;
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = cluster;
@@ -679,11 +671,12 @@ uint32_t clusters_at_once(const void *kernel, uint32_t cluster, uint32_t threads
         cfg.dynamicSmemBytes = smem;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0) have = (uint32_t)n;
+        int v = 0;
+        if (cudaOccupancyMaxActiveClusters(&v, kernel, &cfg) != cudaSuccess || v <= 0) return 0;
+        known[dev][cluster].store((uint32_t)v, std::memory_order_relaxed);
+        return (uint32_t)v;
     }
-    return have;
-}
+};
 // CTAs (or pairs) per tile: enough for `wanted` of them in all, as far as all clusters run at once (a second wave costs more than the split
 // gains: 4096 x 9216 batch 64 by clusters of four, 128 CTAs, 12.4 us; of six and eight, in two waves, 19 and 25).
 template <typename F>
@@ -701,29 +694,32 @@ size_t smem_of(uint32_t split, uint32_t stages)
     return 1024 + (size_t)stages * (LANES + N) * KB + Scales<SWAP, N>::FLOATS * sizeof(float) + sums;
 }
 template <bool SWAP, uint32_t N>
-int launch_fp8(Fp8Args M, const Operands &O, uint32_t wanted, uint32_t stages, cudaStream_t st)
+int launch_fp8(Fp8Args M, const Operands &O, uint32_t wanted, int dev, cudaStream_t st)
 {
+    constexpr uint32_t stages = 4;
+    static AtOnce at_once;
     const uint32_t lane_rows = SWAP ? M.m : M.batch, col_rows = SWAP ? M.batch : M.m;
     const void *const kernel = reinterpret_cast<const void *>(k_fp8_mm<SWAP, N>);
     M.col_tiles = (col_rows + N - 1) / N;
     M.tiles = (lane_rows + LANES - 1) / LANES * M.col_tiles;
     M.stages = stages;
     M.split = split_for(M.tiles, wanted, M.kblocks < 8 ? M.kblocks : 8,
-                        [&](uint32_t s) { return clusters_at_once(kernel, s, threads_of_fp8<N>, smem_of<SWAP, N>(s, stages)); });
+                        [&](uint32_t s) { return at_once(dev, kernel, s, threads_of_fp8<N>, smem_of<SWAP, N>(s, stages)); });
     CUtensorMap wmap, xmap;
     if (!make_map(&wmap, O.w, O.n, M.m, O.ldw, SWAP ? LANES : N) || !make_map(&xmap, O.x, O.n, M.batch, O.ldx, SWAP ? N : LANES)) return SQNN_E_CUDA;
     return launch_clusters(kernel, SWAP ? wmap : xmap, SWAP ? xmap : wmap, M, M.tiles * M.split, M.split, threads_of_fp8<N>,
                            smem_of<SWAP, N>(M.split, stages), st);
 }
 
-int launch_pair(Fp8Args M, const Operands &O, cudaStream_t st)
+int launch_pair(Fp8Args M, const Operands &O, int dev, cudaStream_t st)
 {
+    static AtOnce known[2];                                      // (five and six stages)
     const void *const kernel = reinterpret_cast<const void *>(k_fp8_mm_pair);
     M.col_tiles = (M.m + PAIR_N - 1) / PAIR_N;
     M.tiles = (M.batch + 255) / 256 * M.col_tiles;
     M.stages = M.vec4 ? 6 : 5;
     const size_t smem = 1024 + (size_t)M.stages * PAIR_STAGE + Scales<false, PAIR_N>::FLOATS * sizeof(float) + (M.vec4 ? 0 : PAIR_PW * TURN_FLOATS * sizeof(float));
-    const auto at_once = [&](uint32_t s) { return clusters_at_once(kernel, 2 * s, threads_of_fp8<PAIR_N>, smem); };
+    const auto at_once = [&](uint32_t s) { return known[M.vec4](dev, kernel, 2 * s, threads_of_fp8<PAIR_N>, smem); };
     M.split = split_for(M.tiles, (uint32_t)sm_count() / 2 * 4 / 5, M.kblocks < 4 ? M.kblocks : 4, at_once);
     const uint32_t pairs = at_once(1);
     if (pairs == 0) return SQNN_E_CUDA;
@@ -757,7 +753,6 @@ int fp8_matmul_queue(uint64_t m, uint64_t n, uint32_t batch, const uint8_t *d_w,
     M.status = d_status;
     M.vec4 = ((uintptr_t)d_y % (M.y_bf16 ? 8 : 16)) == 0 && ldy % 4 == 0;
     M.xs_vec = ((uintptr_t)d_x_scale & 15) == 0 && ldxs % 4 == 0;
-    M.prefetch = 1;
     const Operands O{d_w, d_x, ldw, ldx, n};
     const uint64_t w_tiles = (m + LANES - 1) / LANES, x_tiles = ((uint64_t)batch + LANES - 1) / LANES;
     if (w_tiles * x_tiles > 0x7fffffffull / 8) return SQNN_E_UNSUPPORTED;
@@ -765,14 +760,13 @@ int fp8_matmul_queue(uint64_t m, uint64_t n, uint32_t batch, const uint8_t *d_w,
     // Small batches: a quarter more CTAs than SMs keep enough weights on their way; those with more columns are one to an SM.  The pair's larger
     // tiles gain from about as many 128 x 128 tiles on as there are SMs (us, pair / one CTA per tile: 4096 x 16384 batch 512 40.7 / 45.3, 8192 x
     // 1024 batch 2048 35.0 / 40.8; 6000 x 3000 batch 200 15.2 / 11.5, 2048 x 2048 batch 256 11.6 / 7.8).
-    // (Rows of up to 4096 columns leave a CTA few blocks: three stages then let three CTAs onto an SM, the next call's among them: 6000 x 3000 batch 8 6.2 us
-    // against 7.6, 4096 x 9216 batch 1 10.4 against 9.9.)
-    const uint32_t few = M.kblocks <= 32 ? 3 : 4;
-    if (batch <= 16) return launch_fp8<true, 16>(M, O, sms * 5 / 4, few, st);
-    if (batch <= 32) return launch_fp8<true, 32>(M, O, sms * 5 / 4, few, st);
-    if (batch <= 64) return launch_fp8<true, 64>(M, O, sms * 4 / 5, 4, st);
-    if (batch <= 128 || m <= 128 || w_tiles * x_tiles < sms * 4 / 5) return launch_fp8<false, 128>(M, O, sms * 4 / 5, 4, st);
-    return launch_pair(M, O, st);
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SQNN_E_CUDA;
+    if (batch <= 16) return launch_fp8<true, 16>(M, O, sms * 5 / 4, dev, st);
+    if (batch <= 32) return launch_fp8<true, 32>(M, O, sms * 5 / 4, dev, st);
+    if (batch <= 64) return launch_fp8<true, 64>(M, O, sms * 4 / 5, dev, st);
+    if (batch <= 128 || m <= 128 || w_tiles * x_tiles < sms * 4 / 5) return launch_fp8<false, 128>(M, O, sms * 4 / 5, dev, st);
+    return launch_pair(M, O, dev, st);
 }
 
 }  // namespace

@@ -19,9 +19,7 @@
 
 #include <cuda_bf16.h>
 
-#include <map>
-#include <mutex>
-#include <tuple>
+#include <atomic>
 
 namespace sqnn {
 namespace {
@@ -381,18 +379,6 @@ __global__ void __launch_bounds__(512, SLOTS == 1 || (SLOTS == 2 && sizeof(XT) +
     }
 }
 
-// How many blocks run at once (asked for once per kernel, block and device).
-uint32_t blocks_at_once(const void *kernel, uint32_t threads)
-{
-    static std::mutex mu;
-    static std::map<std::tuple<const void *, uint32_t, int>, uint32_t> known;
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return (uint32_t)sm_count();
-    std::lock_guard<std::mutex> lock(mu);
-    uint32_t &have = known[std::make_tuple(kernel, threads, dev)];
-    if (!have) have = (uint32_t)sm_count() * (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, (int)threads, 0) == cudaSuccess && n > 0 ? (uint32_t)n : 1u);
-    return have;
-}
 // Few rows: as many threads as a row has work for (latency); four and more for an SM: two slots a thread or as many as a row needs, so that the reductions
 // weigh less (8192 x 4096, bf16: one slot 84 us, two 58, four 71: two keep 64 registers a thread and so 1024 threads to an SM).
 template <typename XT, typename RT, typename WT, bool RES>
@@ -406,8 +392,22 @@ int launch_norm(const NormArgs &A, uint32_t batch, bool vec, cudaStream_t st)
 #define SQNN_NORM_PICK(S) (vec ? k_rmsnorm_fp8<XT, RT, WT, RES, S, true> : k_rmsnorm_fp8<XT, RT, WT, RES, S, false>)
     auto k = slots == 1 ? SQNN_NORM_PICK(1) : slots == 2 ? SQNN_NORM_PICK(2) : slots == 4 ? SQNN_NORM_PICK(4) : SQNN_NORM_PICK(0);
 #undef SQNN_NORM_PICK
-    const uint32_t at_once = blocks_at_once(reinterpret_cast<const void *>(k), threads);
-    return launch_kernel(k, batch < at_once ? batch : at_once, threads, 0, st, A);
+    // as many blocks as run at once (asked for once per kernel, block and device)
+    const uint32_t sms = (uint32_t)sm_count();
+    uint32_t grid = batch;
+    if (batch > sms) {
+        static std::atomic<uint32_t> known[64][2][4][16];
+        int dev = 0, n = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SQNN_E_CUDA;
+        std::atomic<uint32_t> &have = known[dev][vec][slots == 4 ? 3 : slots][threads / 32 - 1];
+        uint32_t at_once = have.load(std::memory_order_relaxed);
+        if (!at_once) {
+            if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k, (int)threads, 0) != cudaSuccess || n <= 0) return SQNN_E_CUDA;
+            have.store(at_once = sms * (uint32_t)n, std::memory_order_relaxed);
+        }
+        grid = batch < at_once ? batch : at_once;
+    }
+    return launch_kernel(k, grid, threads, 0, st, A);
 }
 template <typename XT, typename RT, bool RES>
 int launch_norm(const NormArgs &A, uint32_t batch, bool w_bf16, bool vec, cudaStream_t st)

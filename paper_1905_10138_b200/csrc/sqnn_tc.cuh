@@ -85,11 +85,6 @@ SQNN_DEV void tma_load_2d_once(uint32_t sdst, const CUtensorMap *map, uint32_t b
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4}], [%2], %5;\n"
                  :: "r"(sdst), "l"(map), "r"(bar), "r"(x), "r"(y), "l"(policy) : "memory");
 }
-// Into L2 only.  Allowed ahead of wait_prior_grid(): L2 is where all writes go, so nothing stale can come of it.
-SQNN_DEV void tma_prefetch_2d(const CUtensorMap *map, int32_t x, int32_t y)
-{
-    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];\n" :: "l"(map), "r"(x), "r"(y) : "memory");
-}
 SQNN_DEV void tmem_alloc(uint32_t *slot, uint32_t cols)
 {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n"
