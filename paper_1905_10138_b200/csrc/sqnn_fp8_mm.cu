@@ -660,7 +660,10 @@ struct AtOnce {
     {
         uint32_t n = known[dev][cluster].load(std::memory_order_relaxed);
         if (n) return n;
-        if (ensure_dynamic_smem(kernel, smem) != SQNN_OK) return 0;
+        // (all of the SM's memory as shared memory: left to itself the runtime may set aside what one CTA needs)
+        if (ensure_dynamic_smem(kernel, smem) != SQNN_OK ||
+            cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
+            return 0;
         cudaLaunchAttribute attr;
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = cluster;
@@ -677,6 +680,13 @@ struct AtOnce {
         return (uint32_t)v;
     }
 };
+// The runtime counts one CTA with tensor memory per SM.  More are there at once where shared and tensor memory allow: 228 KB, of which a CTA
+// takes 1 KB and its static variables besides, and 512 columns.
+constexpr uint32_t ctas_per_sm(size_t smem, uint32_t tmem_cols)
+{
+    const uint32_t by_smem = (uint32_t)(228 * 1024 / (smem + 1536)), by_tmem = 512 / tmem_cols;
+    return by_smem < by_tmem ? by_smem : by_tmem;
+}
 // CTAs (or pairs) per tile: enough for `wanted` of them in all, as far as all clusters run at once (a second wave costs more than the split
 // gains: 4096 x 9216 batch 64 by clusters of four, 128 CTAs, 12.4 us; of six and eight, in two waves, 19 and 25).
 template <typename F>
@@ -704,7 +714,10 @@ int launch_fp8(Fp8Args M, const Operands &O, uint32_t wanted, int dev, cudaStrea
     M.tiles = (lane_rows + LANES - 1) / LANES * M.col_tiles;
     M.stages = stages;
     M.split = split_for(M.tiles, wanted, M.kblocks < 8 ? M.kblocks : 8,
-                        [&](uint32_t s) { return at_once(dev, kernel, s, threads_of_fp8<N>, smem_of<SWAP, N>(s, stages)); });
+                        [&](uint32_t s) {
+                            const size_t smem = smem_of<SWAP, N>(s, stages);
+                            return at_once(dev, kernel, s, threads_of_fp8<N>, smem) * ctas_per_sm(smem, tmem_cols_of<N>);
+                        });
     CUtensorMap wmap, xmap;
     if (!make_map(&wmap, O.w, O.n, M.m, O.ldw, SWAP ? LANES : N) || !make_map(&xmap, O.x, O.n, M.batch, O.ldx, SWAP ? N : LANES)) return SQNN_E_CUDA;
     return launch_clusters(kernel, SWAP ? wmap : xmap, SWAP ? xmap : wmap, M, M.tiles * M.split, M.split, threads_of_fp8<N>,
