@@ -217,11 +217,11 @@ static __device__ __noinline__ float4 ragged4(const float *row, uint32_t at, uin
 }
 SQNN_DEV void raw16(const __nv_bfloat16 *row, uint32_t at, uint32_t n, bool vec, uint32_t (&v)[8])
 {
-    uint4 a, b;
+    uint4 a = make_uint4(0, 0, 0, 0), b = a;
     if (vec && at + 16 <= n) {
         a = *reinterpret_cast<const uint4 *>(row + at);
         b = *reinterpret_cast<const uint4 *>(row + at + 8);
-    } else {
+    } else if (at < n) {
         a = ragged8(row, at, n);
         b = ragged8(row, at + 8, n);
     }
@@ -230,11 +230,11 @@ SQNN_DEV void raw16(const __nv_bfloat16 *row, uint32_t at, uint32_t n, bool vec,
 
 SQNN_DEV void row_values8(const float *row, uint32_t at, uint32_t n, bool vec, float (&v)[8])
 {
-    float4 a, b;
+    float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
     if (vec && at + 8 <= n) {
         a = *reinterpret_cast<const float4 *>(row + at);
         b = *reinterpret_cast<const float4 *>(row + at + 4);
-    } else {
+    } else if (at < n) {
         a = ragged4(row, at, n);
         b = ragged4(row, at + 4, n);
     }
@@ -242,7 +242,7 @@ SQNN_DEV void row_values8(const float *row, uint32_t at, uint32_t n, bool vec, f
 }
 SQNN_DEV void row_values8(const __nv_bfloat16 *row, uint32_t at, uint32_t n, bool vec, float (&v)[8])
 {
-    const uint4 f = vec && at + 8 <= n ? *reinterpret_cast<const uint4 *>(row + at) : ragged8(row, at, n);
+    const uint4 f = vec && at + 8 <= n ? *reinterpret_cast<const uint4 *>(row + at) : at < n ? ragged8(row, at, n) : make_uint4(0, 0, 0, 0);
     const uint32_t u[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
