@@ -37,7 +37,7 @@ namespace {
 
 constexpr uint32_t WARPS = 16, THREADS = WARPS * 32;              // first kernel
 constexpr uint32_t STREAMS = 8;           // its warps that stream weights
-constexpr uint32_t DOWN_WARPS = 12;       // second kernel: all stream
+constexpr uint32_t MAX_DOWN_WARPS = 12;   // second kernel: all stream; 8 where there is no room for the sums and rings of 12
 constexpr uint32_t CLUSTER = 4;           // CTAs that share the routing's work
 constexpr uint32_t STEP = FP8_BLOCK;      // columns per step of a warp
 constexpr uint32_t GROUP = 8;             // tokens multiplied together
@@ -770,7 +770,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
 
 // ---- second kernel: y = sum p D h
 
-template <uint32_t ROWS>
+template <uint32_t ROWS, uint32_t DOWN_WARPS>
 __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_constant__ CUtensorMap weights, const MoeArgs M)
 {
     constexpr uint32_t TILES = ROWS / 16, W_BYTES = ROWS * STEP;
@@ -968,6 +968,12 @@ bool make_map(CUtensorMap *map, const void *p, uint32_t n, uint64_t rows, int64_
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Whether the second kernel has room for a ring of two slots, whatever the call: the sums of all tokens, slots of full groups.
+constexpr bool room_for_down(uint32_t rows, uint32_t warps)
+{
+    return 1024 + warps * (MAX_TOKENS * rows * 4 + 2 * (rows * STEP + GROUP * H_PITCH)) <= DOWN_SMEM_BYTES;
+}
+
 template <typename XT>
 int launch_moe(MoeArgs M, const sqnn_moe *L, cudaStream_t st)
 {
@@ -982,10 +988,14 @@ int launch_moe(MoeArgs M, const sqnn_moe *L, cudaStream_t st)
     // second kernel: 32 rows per CTA where that still makes two CTAs for three SMs; as deep a ring as there is room for
     const uint32_t rows = 3 * ((M.hidden + 31) / 32) >= 2 * (uint32_t)sm_count() ? 32 : 16;
     M.slot = rows * STEP + (M.tokens < M.per ? M.tokens : M.per) * H_PITCH;
-    const size_t sums = (size_t)DOWN_WARPS * M.tokens * rows * 4;
-    M.depth = (uint32_t)((DOWN_SMEM_BYTES - 1024 - sums) / (DOWN_WARPS * M.slot));
-    M.depth = M.depth < MAX_DOWN_DEPTH ? M.depth : MAX_DOWN_DEPTH;
-    const size_t smem_down = 1024 + sums + (size_t)DOWN_WARPS * M.depth * M.slot;
+    // 12 warps with a ring of two slots (16 tokens, 64 experts of 1536, top 8, hidden 4096: 209 us) are faster than 8 with four (213), but do not
+    // always fit; 8 with two do, and so do 12 where a CTA has 16 rows
+    const auto depth_of = [&](uint32_t warps) { return (uint32_t)((DOWN_SMEM_BYTES - 1024 - (size_t)warps * M.tokens * rows * 4) / (warps * M.slot)); };
+    static_assert(room_for_down(16, MAX_DOWN_WARPS) && room_for_down(32, 8), "a ring of two slots whatever the call");
+    const uint32_t warps = depth_of(MAX_DOWN_WARPS) >= 2 ? MAX_DOWN_WARPS : 8;
+    M.depth = depth_of(warps) < MAX_DOWN_DEPTH ? depth_of(warps) : MAX_DOWN_DEPTH;
+    const size_t smem_down = 1024 + (size_t)warps * (M.tokens * rows * 4 + M.depth * M.slot);
+    const auto down = rows == 16 ? k_moe_down<16, MAX_DOWN_WARPS> : warps == 8 ? k_moe_down<32, 8> : k_moe_down<32, MAX_DOWN_WARPS>;
     CUtensorMap gu_map, d_map;
     if (!make_map(&gu_map, L->gate_up, M.hidden, (uint64_t)(M.experts - 1) * M.gu_expert + M.gu_half + M.inner, L->gate_up_row, 16) ||
         !make_map(&d_map, L->down, M.inner, (uint64_t)(M.experts - 1) * M.d_expert + M.hidden, L->down_row, rows))
@@ -1016,7 +1026,7 @@ int launch_moe(MoeArgs M, const sqnn_moe *L, cudaStream_t st)
     cfg.gridDim = dim3((uint32_t)clusters * CLUSTER);
     cfg.numAttrs = 2;
     if (cudaLaunchKernelEx(&cfg, up, gu_map, M) != cudaSuccess) return SQNN_E_CUDA;
-    return launch_kernel(rows == 32 ? k_moe_down<32> : k_moe_down<16>, (M.hidden + rows - 1) / rows, DOWN_WARPS * 32, smem_down, st, d_map, M);
+    return launch_kernel(down, (M.hidden + rows - 1) / rows, warps * 32, smem_down, st, d_map, M);
 }
 
 int moe_queue(const sqnn_moe *L, uint32_t tokens, const void *d_x, int x_dtype, int64_t ldx, void *d_y, int y_dtype, int64_t ldy,

@@ -101,6 +101,16 @@ def test_larger(tokens, experts, top_k, hidden, inner, x_type):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("tokens,experts,top_k,hidden,inner,x_type", [
+    (64, 8, 2, 3200, 400, BF16), (64, 8, 2, 4096, 384, F32), (20, 16, 3, 3300, 256, BF16), (25, 6, 6, 5000, 130, BF16),     # many tokens, wide outputs
+    (32, 512, 16, 256, 128, BF16), (64, 256, 1, 128, 64, F32), (2, 512, 16, 300, 100, F32),                                # most experts, most logits
+    (1, 2, 1, 11264, 300, F32), (3, 4, 2, 11264, 129, BF16), (5, 2, 2, 11264, 11264, F32), (64, 3, 3, 300, 11264, BF16)])  # widest
+def test_limits(tokens, experts, top_k, hidden, inner, x_type):
+    lay, x = layer(experts, hidden, inner, x_type, tokens + inner), tokens_of(tokens, hidden, x_type, 9)
+    check(x, lay, top_k, call(x, lay, top_k))
+
+
+@pytest.mark.gpu
 def test_equal_logits_go_to_the_lowest_index():
     lay = layer(40, 96, 64, F32, 3)
     lay[0][:] = lay[0][0]                                          # all logits equal
