@@ -6,6 +6,7 @@
     python -m paper_1905_10138_b200.profile_case matmul  --cfg 2 --batch 1
     python -m paper_1905_10138_b200.profile_case search  --cfg 2          (exhaustive seed search)
     python -m paper_1905_10138_b200.profile_case case    --name bits_odd  (a listed case of perf/cases.py)
+    python -m paper_1905_10138_b200.profile_case operator --name moe_t1_e64  (a listed case of perf/operators.py)
 
 Run it from the root of the repository.  --cfg 1..4 picks a layer of the benchmark configurations (optionally --rows / --cols smaller),
 --sweep I_S I_M a point of the decode-only sweep (prune rate index, network index).
@@ -30,12 +31,25 @@ def run_case(name: str, iters: int) -> None:
     print(f"{name}: {iters} passes, status {int(state['status'].item()) if 'status' in state else 0}")
 
 
+def run_operator(name: str, iters: int) -> None:
+    """The same for a listed case of the 8-bit operators, with the framework's kernels."""
+    import torch
+    from perf import operators
+    operators.own = True
+    case = next(c for c in operators.listed() if c["name"] == name)
+    state = operators.prepare(case, 7)
+    for _ in range(iters):
+        operators.run(state)
+    torch.cuda.synchronize()
+    print(f"{name}: {iters} passes, status {int(state['status'].item()) if 'status' in state else 0}")
+
+
 def main():
     import torch
     from . import sqnn, workloads as wl
     ap = argparse.ArgumentParser()
-    ap.add_argument("what", choices=["decode", "sink", "bf16", "matmul", "search", "case"])
-    ap.add_argument("--name", help="with `case`: the case's name")
+    ap.add_argument("what", choices=["decode", "sink", "bf16", "matmul", "search", "case", "operator"])
+    ap.add_argument("--name", help="with `case` and `operator`: the case's name")
     ap.add_argument("--cfg", type=int, default=0)
     ap.add_argument("--sweep", type=int, nargs=2, default=None)
     ap.add_argument("--repeat", type=int, default=0,
@@ -48,6 +62,9 @@ def main():
     a = ap.parse_args()
     if a.what == "case":
         run_case(a.name, a.iters)
+        return
+    if a.what == "operator":
+        run_operator(a.name, a.iters)
         return
     if a.sweep is not None:
         layer = wl.make_sweep_layer(a.sweep[0], a.sweep[1], m=a.rows or 32768, n=a.cols or 32768)
