@@ -327,6 +327,7 @@ k_fp8_mm(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ C
     __shared__ uint32_t tmem_slot, abort_word, given_up[8];
     volatile uint32_t *abort_flag = &abort_word;
     bool started = false;                                        // the cluster's first barrier has been waited for
+    bool held = true;                                            // (the issuer's) the tensor memory
     const uint32_t full = smem_addr(bars), empty = full + 8 * MAX_STAGES, acc_full = empty + 8 * MAX_STAGES, acc_empty = acc_full + 8 * 4;
     const uint32_t chunk_bar = acc_empty + 8 * 4, over = chunk_bar + 8;   // scales are there; after a timeout: the MMAs are over
     // [stages][scales][sums of the tile's CTAs]
@@ -446,19 +447,27 @@ k_fp8_mm(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ C
             mma_block(tmem_base + buf * N, a, a + (A_BYTES >> 4), idesc, empty + 8 * stage, acc_full + 8 * buf);
             if (++stage == M.stages) { stage = 0; parity ^= 1u; }
         }
+        // The columns are given back before this CTA waits for others of its cluster, which may be waiting for columns themselves, on an SM that
+        // another kernel shares.
+        for (uint32_t buf = 0; buf < BUFS && buf < it; ++buf)
+            if (!mbar_wait_warp(acc_empty + 8 * buf, ((it - buf + BUFS - 1) / BUFS - 1) & 1u, abort_flag, M.status, M.wait_limit)) goto leave;
+        tc_fence_after();
+        tmem_dealloc(tmem_base, tmem_cols_of<N>);
+        held = false;
     }
 leave:
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (*abort_flag) {                                           // (the same for all: nobody waits any more)
-        if (warp == PW + 1) {                                    // tensor and shared memory must outlive the MMAs that were issued
+        if (warp == PW + 1 && held) {                            // tensor and shared memory must outlive the MMAs that were issued
             mma_commit(over);
             mbar_drain(over, 0, M.wait_limit);
         }
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
+        if (warp == PW + 1 && held) tmem_dealloc(tmem_base, tmem_cols_of<N>);
     }
     if (M.split > 1) {
         if (!started) cluster_wait();
@@ -468,7 +477,6 @@ leave:
         for (uint32_t q = 0; q < M.split; ++q) whole = whole && given_up[q] == 0;
         if (whole) add_sums<SWAP, N, threads_of_fp8<N>>(M, sums, share_of(N, M.split), rank, SWAP ? wblock * FP8_BLOCK : row0, SWAP ? row0 : wblock * FP8_BLOCK, tid);
     }
-    if (warp == PW + 1) tmem_dealloc(tmem_base, tmem_cols_of<N>);
 }
 
 // Tiles of 256 batch rows by 256 weight rows, each by a pair of CTAs (ranks 2 p and 2 p + 1 of a cluster of `split` pairs): this one's 128 batch rows are its

@@ -148,6 +148,21 @@ def test_own_stream_graph_and_two_at_once():
 
 
 @pytest.mark.gpu
+def test_all_forms_at_once_on_streams_of_their_own():
+    """Clusters of several kernels share SMs and their tensor memory."""
+    sizes = [(1000, 6000, 3), (900, 5000, 30), (700, 9000, 60), (500, 7000, 100), (1024, 4000, 700), (8192, 512, 1500)]
+    ops = [operands(*size, 20 + i) for i, size in enumerate(sizes)]
+    want, streams = [product(*o) for o in ops], [torch.cuda.Stream() for _ in ops]
+    outs = [[torch.empty_like(y) for y in want] for _ in range(12)]
+    torch.cuda.synchronize()
+    for row in outs:
+        for o, y, s in zip(ops, row, streams):
+            sqnn.sqnn_fp8_matmul(*o, y, None, s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, w) for row in outs for y, w in zip(row, want))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("m,n,batch", [(300, 4000, 7), (300, 4000, 90), (4096, 300, 2000), (4096, 4000, 500)])
 def test_a_wait_that_gives_up_ends_the_call(m, n, batch):
     ops = operands(m, n, batch, 11)
