@@ -611,48 +611,48 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
     auto join = [&](uint32_t round0, uint32_t round_n, const float *from) {
         const uint32_t k0 = warp - STREAMS;
         if (__any_sync(0xffffffffu, k0 >= round_n || *W.abort_flag)) return;     // (all lanes or none)
-                    const uint32_t unit = round0 + k0, total = round_n * steps;
-                    float sum[8] = {};
-                    for (uint32_t q = 0; q < STREAMS; ++q) {
-                        const uint32_t a = total * q / STREAMS, b = total * (q + 1) / STREAMS;
-                        if (a >= b || b <= k0 * steps || a >= (k0 + 1) * steps) continue;
-                        const float *const p = from + ((q * 2 + (k0 - a / steps)) * 8) * 32 + lane;
-        #pragma unroll
-                        for (uint32_t j = 0; j < 8; ++j) sum[j] += p[j * 32];
+        const uint32_t unit = round0 + k0, total = round_n * steps;
+        float sum[8] = {};
+        for (uint32_t q = 0; q < STREAMS; ++q) {
+            const uint32_t a = total * q / STREAMS, b = total * (q + 1) / STREAMS;
+            if (a >= b || b <= k0 * steps || a >= (k0 + 1) * steps) continue;
+            const float *const p = from + ((q * 2 + (k0 - a / steps)) * 8) * 32 + lane;
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) sum[j] += p[j * 32];
+        }
+        const uint32_t n = unit / per_entry, en = R.entry[n], e = en & 0xffffu, q = unit - n * per_entry, count = tokens_in(n);
+        const uint32_t i = q * 16 + g;                       // rows i and i + 8
+        // where a row's value goes: 16 (row / 4 % 4) + 4 (q % 4) + row % 4 of its 64
+        const uint32_t at = q / (STEP / 16) * H_BLOCK + ((q & 4) * 16 + (g >> 2) * 16 + (q & 3) * 4 + (g & 3)) * 2;
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+            const float a = sum[k], b = sum[2 + k];
+            const float va = i < M.inner ? a / (1.0f + expf(-a)) * sum[4 + k] : 0.0f;
+            const float vb = i + 8 < M.inner ? b / (1.0f + expf(-b)) * sum[6 + k] : 0.0f;
+            uint32_t top = max(__float_as_uint(va) & 0x7fffffffu, __float_as_uint(vb) & 0x7fffffffu);
+#pragma unroll
+            for (uint32_t d = 4; d < 32; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const uint32_t ex = exponent_of(top);
+            const float s = scale_of(ex);
+            const uint32_t hi = f16x2(va * s, vb * s), lo = f16x2(va * s - f16_lo(hi), vb * s - f16_hi(hi));
+            const uint32_t column = 2 * t4 + k;
+            if (column < count) {
+                const uint32_t t = token_of(R, e, (en >> 16) * M.per + column);
+                uint8_t *const row = M.h + (uint64_t)pair_of(R, M, t, e) * M.h_row;
+                *reinterpret_cast<uint16_t *>(row + at) = (uint16_t)hi;
+                *reinterpret_cast<uint16_t *>(row + at + 64) = (uint16_t)(hi >> 16);
+                *reinterpret_cast<uint16_t *>(row + at + 256) = (uint16_t)lo;
+                *reinterpret_cast<uint16_t *>(row + at + 320) = (uint16_t)(lo >> 16);
+                if (g == 0) *reinterpret_cast<float *>(row + q / 8 * H_BLOCK + 512 + (q & 7) * 4) = back_of(ex);
+                if (q + 1 == per_entry)                      // the rest of the last block is zero
+                    for (uint32_t z = q + 1; z & 7; ++z) {
+                        const uint32_t to = z / 8 * H_BLOCK + ((z & 4) * 16 + (g >> 2) * 16 + (z & 3) * 4 + (g & 3)) * 2;
+                        *reinterpret_cast<uint16_t *>(row + to) = *reinterpret_cast<uint16_t *>(row + to + 64) = 0;
+                        *reinterpret_cast<uint16_t *>(row + to + 256) = *reinterpret_cast<uint16_t *>(row + to + 320) = 0;
+                        if (g == 0) *reinterpret_cast<float *>(row + z / 8 * H_BLOCK + 512 + (z & 7) * 4) = 0.0f;
                     }
-                    const uint32_t n = unit / per_entry, en = R.entry[n], e = en & 0xffffu, q = unit - n * per_entry, count = tokens_in(n);
-                    const uint32_t i = q * 16 + g;                       // rows i and i + 8
-                    // where a row's value goes: 16 (row / 4 % 4) + 4 (q % 4) + row % 4 of its 64
-                    const uint32_t at = q / (STEP / 16) * H_BLOCK + ((q & 4) * 16 + (g >> 2) * 16 + (q & 3) * 4 + (g & 3)) * 2;
-        #pragma unroll
-                    for (uint32_t k = 0; k < 2; ++k) {
-                        const float a = sum[k], b = sum[2 + k];
-                        const float va = i < M.inner ? a / (1.0f + expf(-a)) * sum[4 + k] : 0.0f;
-                        const float vb = i + 8 < M.inner ? b / (1.0f + expf(-b)) * sum[6 + k] : 0.0f;
-                        uint32_t top = max(__float_as_uint(va) & 0x7fffffffu, __float_as_uint(vb) & 0x7fffffffu);
-        #pragma unroll
-                        for (uint32_t d = 4; d < 32; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-                        const uint32_t ex = exponent_of(top);
-                        const float s = scale_of(ex);
-                        const uint32_t hi = f16x2(va * s, vb * s), lo = f16x2(va * s - f16_lo(hi), vb * s - f16_hi(hi));
-                        const uint32_t column = 2 * t4 + k;
-                        if (column < count) {
-                            const uint32_t t = token_of(R, e, (en >> 16) * M.per + column);
-                            uint8_t *const row = M.h + (uint64_t)pair_of(R, M, t, e) * M.h_row;
-                            *reinterpret_cast<uint16_t *>(row + at) = (uint16_t)hi;
-                            *reinterpret_cast<uint16_t *>(row + at + 64) = (uint16_t)(hi >> 16);
-                            *reinterpret_cast<uint16_t *>(row + at + 256) = (uint16_t)lo;
-                            *reinterpret_cast<uint16_t *>(row + at + 320) = (uint16_t)(lo >> 16);
-                            if (g == 0) *reinterpret_cast<float *>(row + q / 8 * H_BLOCK + 512 + (q & 7) * 4) = back_of(ex);
-                            if (q + 1 == per_entry)                      // the rest of the last block is zero
-                                for (uint32_t z = q + 1; z & 7; ++z) {
-                                    const uint32_t to = z / 8 * H_BLOCK + ((z & 4) * 16 + (g >> 2) * 16 + (z & 3) * 4 + (g & 3)) * 2;
-                                    *reinterpret_cast<uint16_t *>(row + to) = *reinterpret_cast<uint16_t *>(row + to + 64) = 0;
-                                    *reinterpret_cast<uint16_t *>(row + to + 256) = *reinterpret_cast<uint16_t *>(row + to + 320) = 0;
-                                    if (g == 0) *reinterpret_cast<float *>(row + z / 8 * H_BLOCK + 512 + (z & 7) * 4) = 0.0f;
-                                }
-                        }
-                    }
+            }
+        }
     };
     Walk w;
     w.window1 = w.round_n = 0;
@@ -737,7 +737,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
                     if constexpr (PIECES == 2) mma_f16(cu[p & 1], a, lo.z, lo.w);
                 }
                 __syncwarp();                                    // the slot has been read
-                // (asked for three steps ahead: with a ring of four, into the slot before this one, free since the last step)
+                // (three steps ahead: into the slot before this one, free since the last step)
                 request();
                 if (++get_slot == UP_DEPTH) { get_slot = 0; get_parity ^= 1; }
 #pragma unroll
@@ -1051,8 +1051,9 @@ int moe_queue(const sqnn_moe *L, uint32_t tokens, const void *d_x, int x_dtype, 
         return SQNN_E_INVALID_ARG;
     if (!aligned_to(L->gate_up, 16) || !aligned_to(L->down, 16) || ((L->gate_up_row | L->down_row) & 15)) return SQNN_E_UNSUPPORTED;
     // the weights of all experts are rows of one matrix to the copies
-    const int64_t most_rows = 1ll << 30;
-    if (L->gate_up_half % L->gate_up_row || L->gate_up_expert % L->gate_up_row || L->down_expert % L->down_row || L->gate_up_row > (1ll << 30) || L->down_row > (1ll << 30) ||
+    const int64_t most_rows = 1ll << 30, most_elements = 1ll << 50;      // (what is multiplied below stays within 64 bits)
+    if (L->gate_up_expert > most_elements || L->gate_up_half > most_elements || L->down_expert > most_elements ||
+        L->gate_up_half % L->gate_up_row || L->gate_up_expert % L->gate_up_row || L->down_expert % L->down_row || L->gate_up_row > (1ll << 30) || L->down_row > (1ll << 30) ||
         L->gate_up_expert / L->gate_up_row * L->experts + L->gate_up_half / L->gate_up_row + inner > most_rows || L->down_expert / L->down_row * L->experts + hidden > most_rows)
         return SQNN_E_UNSUPPORTED;
     const MoeShape shape = moe_shape(tokens, L->top_k, L->inner);
@@ -1086,7 +1087,7 @@ int moe_queue(const sqnn_moe *L, uint32_t tokens, const void *d_x, int x_dtype, 
 
 extern "C" size_t sqnn_moe_workspace_bytes(uint32_t tokens, uint32_t top_k, uint32_t inner)
 {
-    if (tokens > SQNN_MOE_MAX_TOKENS || top_k > SQNN_MOE_MAX_TOP_K) return 0;
+    if (tokens > SQNN_MOE_MAX_TOKENS || top_k > SQNN_MOE_MAX_TOP_K || inner > SQNN_MOE_MAX_WIDTH) return 0;
     return sqnn::moe_shape(tokens, top_k, inner).bytes;
 }
 

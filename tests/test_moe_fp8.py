@@ -270,14 +270,15 @@ def test_refusals_of_the_c_entry_point():
                 dict(down=None), dict(down_scale=None), dict(router_row=255), dict(gate_up_row=240), dict(down_row=112), dict(gate_up_half=-16),
                 dict(gate_up_expert=-16), dict(down_expert=-16), dict(gate_up_scale=4098), dict(down_scale=4097), dict(router=4097)):
         assert rc(c_layer(**bad)) == sqnn.E_INVALID_ARG, bad
-    for bad in (dict(experts=513), dict(top_k=17, experts=32), dict(gate_up=4104), dict(down=4100), dict(gate_up_row=264), dict(down_row=136), dict(gate_up_half=32784), dict(gate_up_expert=65600), dict(down_expert=32784),
+    for bad in (dict(experts=513), dict(top_k=17, experts=32), dict(gate_up=4104), dict(down=4100), dict(gate_up_row=264), dict(down_row=136), dict(gate_up_half=32784), dict(gate_up_expert=65600), dict(down_expert=32784), dict(gate_up_expert=1 << 60), dict(gate_up_half=1 << 60),
+                dict(down_expert=1 << 60),
                 dict(hidden=(1 << 20) + 1, router_row=1 << 21, gate_up_row=1 << 21), dict(inner=(1 << 20) + 1, down_row=1 << 21)):
         lay = c_layer(**bad)
         assert rc(lay, ldx=1 << 21, ldy=1 << 21) == sqnn.E_UNSUPPORTED, bad
     assert rc(tokens=65) == sqnn.E_UNSUPPORTED
     assert rc(c_layer(experts=300), tokens=64) == sqnn.E_UNSUPPORTED
     need = sqnn.sqnn_moe_workspace_bytes(4, 2, 128)
-    assert need > 0 and sqnn.sqnn_moe_workspace_bytes(65, 2, 128) == 0
+    assert need > 0 and sqnn.sqnn_moe_workspace_bytes(65, 2, 128) == 0 and sqnn.sqnn_moe_workspace_bytes(4, 2, 11265) == 0
     for bad in (dict(ws=None), dict(bytes=need - 1), dict(ws=65536 + 128)):
         assert rc(**bad) == sqnn.E_WORKSPACE, bad
 
