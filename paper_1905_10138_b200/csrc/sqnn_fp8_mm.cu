@@ -16,6 +16,10 @@
 // Few tiles: the CTAs of a cluster share one, each taking a range of the blocks k; each sends its sums to the CTAs that own a share of the
 // columns, through distributed shared memory, and these add them up in the order of the ranks.  No workspace, no atomics: results are the same
 // from run to run.
+//
+// Measured (floor at the copy's and the tensor cores' measured rates): 4096 x 9216 batch 1 9.9 us (5.8), batch 64 12.5 us (6.0), 4096 x 16384 batch 512
+// 49 us (20.6), batch 4096 323 us (164).  Small batches are bound by how soon the loads start and by the end of the call (start, exchange of sums) beside the
+// stream; large ones by the two accumulators that take turns: per two blocks 600 cycles of MMA, and reading, scaling and signalling 1200 that overlap only in part.
 #include "sqnn_launch.h"
 #include "sqnn_fp8.cuh"
 #include "sqnn_cluster.cuh"
