@@ -183,15 +183,16 @@ static __device__ __noinline__ uint2 convert_exactly(float4 a, float4 b, float4 
 }
 
 // A block takes rows in turn; SLOTS slots of eight elements a thread stay in registers, and the next row is on its way while this one is
-// finished.  SLOTS = 0: rows longer than that are read a second time, h where it was stored.
-template <typename XT, typename RT, typename WT, bool RES, uint32_t SLOTS, bool VEC>
-__global__ void __launch_bounds__(512, SLOTS == 1 || (SLOTS == 2 && sizeof(XT) + (RES ? sizeof(RT) : 0) <= 4) ? 2 : 1) k_rmsnorm_fp8(const NormArgs A)
+// finished.  SLOTS = 0: rows longer than that are read a second time, h where it was stored.  MOST = 384 with one slot: three blocks to an SM hide what a
+// look ahead would, and take fewer registers.
+template <typename XT, typename RT, typename WT, bool RES, uint32_t SLOTS, uint32_t MOST, bool VEC>
+__global__ void __launch_bounds__(MOST, MOST == 384 ? 3 : SLOTS == 1 || (SLOTS == 2 && (!VEC || sizeof(XT) + (RES ? sizeof(RT) : 0) <= 4)) ? 2 : 1) k_rmsnorm_fp8(const NormArgs A)
 {
     __shared__ double part[16];
     __shared__ double rstd_s;
     constexpr bool EXACT = sizeof(RT) == 2 && sizeof(WT) == 2;     // products of h and w are fp32 numbers
     constexpr uint32_t KEPT = SLOTS ? SLOTS : 1;
-    constexpr bool AHEAD = SLOTS * (sizeof(XT) + (RES ? sizeof(RT) : 0)) <= 16;      // what registers allow (SLOTS = 0: nothing to ask for)
+    constexpr bool AHEAD = MOST == 512 && SLOTS * (sizeof(XT) + (RES ? sizeof(RT) : 0)) <= 16;      // what registers allow (SLOTS = 0: nothing to ask for)
     constexpr bool KEEP_WEIGHTS = SLOTS > 0 && sizeof(WT) == 2;
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, T = blockDim.x, n = A.n, units = (n + 127) / 128 * 16;
     wait_prior_grid();
@@ -379,18 +380,23 @@ __global__ void __launch_bounds__(512, SLOTS == 1 || (SLOTS == 2 && sizeof(XT) +
     }
 }
 
-// Few rows: as many threads as a row has work for (latency); four and more for an SM: two slots a thread or as many as a row needs, so that the reductions
-// weigh less (8192 x 4096, bf16: one slot 84 us, two 58, four 71: two keep 64 registers a thread and so 1024 threads to an SM).
+// One slot of eight elements a thread, as far as 512 threads go, else as many as a row needs.  Many rows of which a thread loads no more than four bytes an
+// element, on 16-byte boundaries: two slots, so that the reductions weigh less (8192 x 4096, bf16 with residual: one slot 59 us, two 56, four 71; at 2000 rows
+// 17.3 and 18.7; 8000 x 2944 52 and 46, 2000 x 2944 16.3 and 15.4).  fp32 or unaligned rows have no registers to spare for two (8000 x 3001, fp32 and bf16 residual, bf16 y: 96 us
+// with one, 166 with two; 8000 x 4096 66 and 76).  Where unaligned rows need two slots, two blocks to an SM (2000 x 5001, the same types: 58 us, one block 88).
 template <typename XT, typename RT, typename WT, bool RES>
 int launch_norm(const NormArgs &A, uint32_t batch, bool vec, cudaStream_t st)
 {
     const uint32_t units = (A.n + 127) / 128 * 16, most = 512;
     const uint32_t least = units <= most ? 1 : units <= 2 * most ? 2 : units <= 4 * most ? 4 : 0;
-    const uint32_t slots = least == 0 ? 0 : batch < 4 * (uint32_t)sm_count() || units <= 128 ? least : least <= 2 ? 2 : 4;
+    const bool light = vec && sizeof(XT) + (RES ? sizeof(RT) : 0) <= 4;
+    const bool many = batch >= (units <= 384 ? 4 : 16) * (uint32_t)sm_count();
+    const uint32_t slots = least == 1 && light && many && units > 128 ? 2 : least;
     const uint32_t per = slots ? (units + slots - 1) / slots : most;
     const uint32_t threads = (per + 31) / 32 * 32;
-#define SQNN_NORM_PICK(S) (vec ? k_rmsnorm_fp8<XT, RT, WT, RES, S, true> : k_rmsnorm_fp8<XT, RT, WT, RES, S, false>)
-    auto k = slots == 1 ? SQNN_NORM_PICK(1) : slots == 2 ? SQNN_NORM_PICK(2) : slots == 4 ? SQNN_NORM_PICK(4) : SQNN_NORM_PICK(0);
+#define SQNN_NORM_PICK(S, T) (vec ? k_rmsnorm_fp8<XT, RT, WT, RES, S, T, true> : k_rmsnorm_fp8<XT, RT, WT, RES, S, T, false>)
+    auto k = slots == 1 ? threads <= 384 ? SQNN_NORM_PICK(1, 384) : SQNN_NORM_PICK(1, 512) : slots == 2 ? SQNN_NORM_PICK(2, 512)
+           : slots == 4 ? SQNN_NORM_PICK(4, 512) : SQNN_NORM_PICK(0, 512);
 #undef SQNN_NORM_PICK
     // as many blocks as run at once (asked for once per kernel, block and device)
     const uint32_t sms = (uint32_t)sm_count();
