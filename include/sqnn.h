@@ -370,7 +370,7 @@ void sqnn_set_debug_flags(uint32_t flags, uint64_t wait_limit_cycles);
  * d_residual and d_h: both or neither, of residual_dtype.  d_q with d_scale ([batch][ceil(n / 128)], row
  * stride lds), or d_y (y_dtype), or all three are written.  Types SQNN_X_F32 or SQNN_X_BF16 (the fp32 output
  * of the products is a valid x beside a bf16 residual).  h, scale and q are what the formulas give in exact
- * arithmetic, whatever the sizes (but for values within 2^-50 or so of a border), so results do not depend on the order of a
+ * arithmetic, whatever the sizes (but for values within 2^-50 or so of a border; |y| within 2^-100 .. 2^127), so results do not depend on the order of a
  * sum; y is within two last places of fp32, rounded to its type.  A NaN or an infinity
  * in a row of h makes NaN of its columns' groups (scale and q) and of y there; what else is in
  * such a row follows from the formulas.  d_h may be d_residual or d_x and d_y may be d_x where type and
@@ -389,7 +389,7 @@ int sqnn_rmsnorm_fp8(uint32_t batch, uint64_t n, const void *d_x, int x_dtype, i
  * batch rows of m, row stride ldy, y_dtype SQNN_X_F32 or SQNN_X_BF16 (rounded once, at the end); fully
  * overwritten, nothing beside the rows is touched.  Any m, n and batch from 1 on.  Sums are kept in fp32: over
  * 128 columns in tensor memory, then scaled and added in registers, in a fixed order: results are bit-identical from run to
- * run.  What is not finite goes through as in that sum.  One kernel, no workspace, nothing allocated.
+ * run.  What is not finite goes through as in that sum.  One kernel or two, no workspace, nothing allocated.
  * W and X need a 16-byte aligned base and row strides that are multiples of 16 (what lies between n and the
  * stride is not used).  Errors: INVALID_ARG (NULL, sizes, strides, types), UNSUPPORTED (W or X
  * not on 16-byte boundaries, m, n or batch above 2^30), CUDA; d_status as for the products. */

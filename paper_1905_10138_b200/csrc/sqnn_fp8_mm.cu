@@ -18,7 +18,7 @@
 // from run to run.
 //
 // Measured (floor at the copy's and the tensor cores' measured rates): 4096 x 9216 batch 1 9.9 us (5.8), batch 64 12.5 us (6.0), 4096 x 16384 batch 512
-// 49 us (20.6), batch 4096 323 us (164).  Small batches are bound by how soon the loads start and by the end of the call (start, exchange of sums) beside the
+// 49 us (20.6), batch 4096 299 to 312 us (164).  Small batches are bound by how soon the loads start and by the end of the call (start, exchange of sums) beside the
 // stream; large ones by the two accumulators that take turns: per two blocks 600 cycles of MMA, and reading, scaling and signalling 1200 that overlap only in part.
 #include "sqnn_launch.h"
 #include "sqnn_fp8.cuh"
@@ -47,6 +47,7 @@ struct Fp8Args {
     uint32_t kblocks;             // blocks of 128 columns per row
     uint32_t tiles, col_tiles;    // tiles in all; tiles along the columns
     uint32_t split;               // CTAs per tile (= cluster size)
+    uint32_t quarters, first;     // tiles are quarters of the pair's tiles (`col_tiles` of them along the columns) from `first` on
     uint32_t stages;
     uint32_t y_bf16, vec, vec4;   // rows of Y on 16-byte boundaries; on those of four elements
     uint32_t xs_vec;              // rows of the activations' scales on 16-byte boundaries
@@ -341,7 +342,14 @@ k_fp8_mm(const __grid_constant__ CUtensorMap lane_map, const __grid_constant__ C
     sc.buf = after;
     float *const sums = after + Scales<SWAP, N>::FLOATS;
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t rank = M.split > 1 ? cluster_rank() : 0, tile = blockIdx.x / M.split, tl = tile / M.col_tiles, tc = tile - tl * M.col_tiles;
+    const uint32_t rank = M.split > 1 ? cluster_rank() : 0, tile = blockIdx.x / M.split;
+    uint32_t tl = tile / M.col_tiles, tc = tile - tl * M.col_tiles;
+    if (!SWAP && M.quarters) {
+        const uint32_t whole = M.first + tile / 4;
+        tl = whole / M.col_tiles;
+        tc = 2 * (whole - tl * M.col_tiles) + (tile & 1);
+        tl = 2 * tl + (tile >> 1 & 1);
+    }
     const uint32_t k_begin = M.kblocks * rank / M.split, k_end = M.kblocks * (rank + 1) / M.split;
     const uint32_t k_first = k_begin & ~3u;                      // where the first chunk of scales begins
     // first batch row of the scales, first block of weight rows
@@ -722,8 +730,10 @@ int launch_fp8(Fp8Args M, const Operands &O, uint32_t wanted, int dev, cudaStrea
     static AtOnce at_once;
     const uint32_t lane_rows = SWAP ? M.m : M.batch, col_rows = SWAP ? M.batch : M.m;
     const void *const kernel = reinterpret_cast<const void *>(k_fp8_mm<SWAP, N>);
-    M.col_tiles = (col_rows + N - 1) / N;
-    M.tiles = (lane_rows + LANES - 1) / LANES * M.col_tiles;
+    if (!M.quarters) {
+        M.col_tiles = (col_rows + N - 1) / N;
+        M.tiles = (lane_rows + LANES - 1) / LANES * M.col_tiles;
+    }
     M.stages = stages;
     M.split = split_for(M.tiles, wanted, M.kblocks < 8 ? M.kblocks : 8,
                         [&](uint32_t s) {
@@ -750,8 +760,19 @@ int launch_pair(Fp8Args M, const Operands &O, int dev, cudaStream_t st)
     if (pairs == 0) return SQNN_E_CUDA;
     CUtensorMap wmap, xmap;
     if (!make_map(&wmap, O.w, O.n, M.m, O.ldw, LANES) || !make_map(&xmap, O.x, O.n, M.batch, O.ldx, LANES)) return SQNN_E_CUDA;
+    // Tiles of a last round that would leave most pairs idle are done as quarters, a CTA or a cluster each, by a kernel of their own (us, without / with:
+    // 4096 x 9216 batch 1300, 22 of 96 tiles, 81.5 / 72.3; 2560 x 4096 batch 2048, 6 of 80, 46.5 / 39.5; 34 of 256 tiles: 4096 x 16384 batch
+    // 4096 308 / 299, 4096 x 9216 180 / 173, but 8192 x 1024 batch 2048 37 / 39, so short rows keep to two thirds of the SMs).
+    const uint32_t last = M.split == 1 && M.tiles > pairs ? M.tiles % pairs : 0;
+    const bool tail = last > 0 && 4 * last <= (M.kblocks < 64 ? (uint32_t)sm_count() * 2 / 3 : (uint32_t)sm_count());
+    if (tail) M.tiles -= last;
     const uint32_t clusters = M.split > 1 || M.tiles < pairs ? M.tiles : pairs;
-    return launch_clusters(kernel, xmap, wmap, M, clusters * 2 * M.split, 2 * M.split, threads_of_fp8<PAIR_N>, smem, st);
+    const int rc = launch_clusters(kernel, xmap, wmap, M, clusters * 2 * M.split, 2 * M.split, threads_of_fp8<PAIR_N>, smem, st);
+    if (rc != SQNN_OK || !tail) return rc;
+    M.quarters = 1;
+    M.first = M.tiles;
+    M.tiles = 4 * last;
+    return launch_fp8<false, 128>(M, O, (uint32_t)sm_count() * 4 / 5, dev, st);
 }
 
 int fp8_matmul_queue(uint64_t m, uint64_t n, uint32_t batch, const uint8_t *d_w, int64_t ldw, const float *d_w_scale, int64_t ldws,

@@ -148,6 +148,13 @@ def test_own_stream_graph_and_two_at_once():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("m,n,batch,y_type,pad", [(2560, 256, 2048, F32, 0), (2430, 700, 2020, BF16, 3), (2305, 1300, 1793, F32, 1), (256, 130, 19200, BF16, 0),
+                                                  (8192, 300, 1200, BF16, 8), (300, 2000, 9601, F32, 0)])
+def test_tiles_of_a_last_round(m, n, batch, y_type, pad):
+    run(m, n, batch, y_type, pad)
+
+
+@pytest.mark.gpu
 def test_all_forms_at_once_on_streams_of_their_own():
     """Clusters of several kernels share SMs and their tensor memory."""
     sizes = [(1000, 6000, 3), (900, 5000, 30), (700, 9000, 60), (500, 7000, 100), (1024, 4000, 700), (8192, 512, 1500)]
