@@ -20,8 +20,8 @@
 //
 // k_moe_up:   every cluster works out the routing for itself (its CTAs share the experts' logits through distributed shared memory), then the CTAs
 //             share all units (expert, 16 rows of G and the same of U); a CTA's warps share the columns of up to 16 units at a time.
-// k_moe_down: a CTA has 16 or 32 rows of all chosen experts' D; its warps share (expert, 128 columns) evenly; each sums into its own
-//             accumulators, which are added up in warp order.
+// k_moe_down: a CTA, or a cluster of two or four, has 16 or 32 rows of all chosen experts' D; the warps share (expert, 128 columns) evenly; each sums into its own
+//             accumulators, which are added up in warp and rank order.
 // No atomics on sums: results are the same from run to run.
 #include "sqnn_launch.h"
 #include "sqnn_fp8.cuh"
@@ -80,6 +80,7 @@ struct MoeArgs {
     uint32_t x_row, x_rows;       // first kernel: bytes per staged row of x, how many there is room for
     uint32_t per;                 // tokens per entry in the first kernel
     uint32_t depth, slot;         // second kernel's ring
+    uint32_t split;               // its CTAs (a cluster) that share a run of rows
     uint32_t skip_loads;          // test only: no weights are asked for
     uint64_t wait_limit;
     uint32_t *status;
@@ -770,7 +771,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
 
 // ---- second kernel: y = sum p D h
 
-template <uint32_t ROWS, uint32_t DOWN_WARPS>
+template <uint32_t ROWS, uint32_t DOWN_WARPS, bool SPLIT>
 __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_constant__ CUtensorMap weights, const MoeArgs M)
 {
     constexpr uint32_t TILES = ROWS / 16, W_BYTES = ROWS * STEP;
@@ -785,7 +786,7 @@ __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_co
     const uint32_t h_ring = smem_addr(smem) + DOWN_WARPS * M.depth * W_BYTES + warp * M.depth * h_slot, my_bars = smem_addr(bars) + 8 * warp * MAX_DOWN_DEPTH;
     float *const sums = reinterpret_cast<float *>(smem + (size_t)DOWN_WARPS * M.depth * M.slot);
     float *const mine = sums + warp * M.tokens * ROWS;
-    const uint32_t row0 = blockIdx.x * ROWS;
+    const uint32_t rank = SPLIT ? cluster_rank() : 0, row0 = (SPLIT ? blockIdx.x / M.split : blockIdx.x) * ROWS;
     const Waits W{&abort_word, M.status, M.wait_limit};
     for (uint32_t i = lane; i < M.tokens * ROWS; i += 32) mine[i] = 0.0f;
     if (lane < M.depth) mbar_init(my_bars + 8 * lane, 1);
@@ -803,7 +804,8 @@ __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_co
     __syncthreads();
     auto entry = [&](uint32_t n) -> const Entry & { return n < NEAR_ENTRIES ? near[n] : M.list[n]; };
     const uint32_t steps = (M.inner + STEP - 1) / STEP, total = list_size * steps;
-    const uint32_t q0 = total * warp / DOWN_WARPS, q1 = total * (warp + 1) / DOWN_WARPS;
+    const uint32_t part = rank * DOWN_WARPS + warp, parts = SPLIT ? M.split * DOWN_WARPS : DOWN_WARPS;
+    const uint32_t q0 = total * part / parts, q1 = total * (part + 1) / parts;
 
     // ---- a step's weights and its tokens' inner values into the rings
     uint32_t ahead_n = q0 / steps, ahead_c = q0 - ahead_n * steps, ahead_q = q0, put_slot = 0, issued = 0;
@@ -929,19 +931,33 @@ __global__ void __launch_bounds__(DOWN_WARPS * 32, 1) k_moe_down(const __grid_co
                 const uint32_t uses = (issued + M.depth - 1 - s) / M.depth;
                 if (uses) mbar_drain(my_bars + 8 * s, (uses - 1) & 1u, M.wait_limit);
             }
-        return;
+        if (!SPLIT) return;                                      // (the others of a cluster look at the flag)
     }
+    auto write = [&](uint32_t i, float s) {
+        const uint32_t row = row0 + i % ROWS;
+        if (row >= M.hidden) return;
+        const int64_t at = (int64_t)(i / ROWS) * M.ldy + row;
+        if (M.y_bf16) static_cast<__nv_bfloat16 *>(M.y)[at] = __float2bfloat16_rn(s);
+        else static_cast<float *>(M.y)[at] = s;
+    };
     for (uint32_t i = tid; i < M.tokens * ROWS; i += DOWN_WARPS * 32) {
-        const uint32_t t = i / ROWS, row = row0 + i % ROWS;
         float s = 0.0f;
 #pragma unroll
         for (uint32_t w = 0; w < DOWN_WARPS; ++w) s += sums[w * M.tokens * ROWS + i];
-        if (row < M.hidden) {
-            const int64_t at = (int64_t)t * M.ldy + row;
-            if (M.y_bf16) static_cast<__nv_bfloat16 *>(M.y)[at] = __float2bfloat16_rn(s);
-            else static_cast<float *>(M.y)[at] = s;
-        }
+        if (!SPLIT) write(i, s);
+        else sums[i] = s;                                        // (nobody else reads this place)
     }
+    if constexpr (!SPLIT) return;
+    __syncwarp();
+    cluster_sync();                                              // all CTAs' sums are there; each adds up a share, in rank order
+    bool whole = true;
+    for (uint32_t r = 0; r < M.split; ++r) whole = whole && peer_load(peer_addr(smem_addr(&abort_word), r)) == 0;
+    for (uint32_t i = rank * DOWN_WARPS * 32 + tid; whole && i < M.tokens * ROWS; i += parts * 32) {
+        float s = 0.0f;
+        for (uint32_t r = 0; r < M.split; ++r) s += __uint_as_float(peer_load(peer_addr(smem_addr(sums + i), r)));
+        write(i, s);
+    }
+    cluster_sync();                                              // shared memory outlives its readers
 }
 
 // ---- host
@@ -995,7 +1011,8 @@ int launch_moe(MoeArgs M, const sqnn_moe *L, cudaStream_t st)
     const uint32_t warps = depth_of(MAX_DOWN_WARPS) >= 2 ? MAX_DOWN_WARPS : 8;
     M.depth = depth_of(warps) < MAX_DOWN_DEPTH ? depth_of(warps) : MAX_DOWN_DEPTH;
     const size_t smem_down = 1024 + (size_t)warps * (M.tokens * rows * 4 + M.depth * M.slot);
-    const auto down = rows == 16 ? k_moe_down<16, MAX_DOWN_WARPS> : warps == 8 ? k_moe_down<32, 8> : k_moe_down<32, MAX_DOWN_WARPS>;
+    const auto down = rows == 16 ? k_moe_down<16, MAX_DOWN_WARPS, false> : warps == 8 ? k_moe_down<32, 8, false> : k_moe_down<32, MAX_DOWN_WARPS, false>;
+    const auto down_split = k_moe_down<16, MAX_DOWN_WARPS, true>;
     CUtensorMap gu_map, d_map;
     if (!make_map(&gu_map, L->gate_up, M.hidden, (uint64_t)(M.experts - 1) * M.gu_expert + M.gu_half + M.inner, L->gate_up_row, 16) ||
         !make_map(&d_map, L->down, M.inner, (uint64_t)(M.experts - 1) * M.d_expert + M.hidden, L->down_row, rows))
@@ -1025,8 +1042,39 @@ int launch_moe(MoeArgs M, const sqnn_moe *L, cudaStream_t st)
     }
     cfg.gridDim = dim3((uint32_t)clusters * CLUSTER);
     cfg.numAttrs = 2;
+    // Few runs of rows: a cluster shares one, as far as all clusters run at once and each warp has three steps or more (29 tokens, 7 of 8 experts, hidden 367,
+    // inner 3264: 121 us by one CTA a run, 73 by four; 5 tokens, 3 of 12, 1000 and 500, two steps a warp: 20.5 and 21.3).
+    const uint32_t runs = (M.hidden + rows - 1) / rows, steps = (M.inner + STEP - 1) / STEP, reached = M.tokens * M.top_k < M.experts ? M.tokens * M.top_k : M.experts;
+    cudaLaunchConfig_t cfg_down = cfg;
+    cudaLaunchAttribute attr_down[2] = {attr[0], attr[1]};
+    cfg_down.attrs = attr_down;
+    cfg_down.blockDim = dim3(warps * 32);
+    M.split = 1;
+    if (rows == 16) {
+        static std::atomic<int> known_down[64][2];
+        for (uint32_t s = 4; s > 1 && M.split == 1; s /= 2) {            // (three: 46 us where two take 42)
+            if (runs * s > (uint32_t)sm_count() || reached * steps < 3 * s * warps) continue;
+            int at_once = dev < 64 ? known_down[dev][s / 4].load(std::memory_order_relaxed) : 0;
+            if (at_once == 0) {
+                if (ensure_dynamic_smem(reinterpret_cast<const void *>(down_split), DOWN_SMEM_BYTES) != SQNN_OK) return SQNN_E_CUDA;
+                attr_down[0].val.clusterDim.x = s;
+                cfg_down.gridDim = dim3(s);
+                cfg_down.numAttrs = 1;
+                cfg_down.dynamicSmemBytes = DOWN_SMEM_BYTES;
+                if (cudaOccupancyMaxActiveClusters(&at_once, down_split, &cfg_down) != cudaSuccess || at_once <= 0) return SQNN_E_CUDA;
+                if (dev < 64) known_down[dev][s / 4].store(at_once, std::memory_order_relaxed);
+            }
+            if (runs <= (uint32_t)at_once) M.split = s;
+        }
+    }
     if (cudaLaunchKernelEx(&cfg, up, gu_map, M) != cudaSuccess) return SQNN_E_CUDA;
-    return launch_kernel(down, (M.hidden + rows - 1) / rows, warps * 32, smem_down, st, d_map, M);
+    if (M.split == 1) return launch_kernel(down, runs, warps * 32, smem_down, st, d_map, M);
+    if (ensure_dynamic_smem(reinterpret_cast<const void *>(down_split), smem_down) != SQNN_OK) return SQNN_E_CUDA;
+    attr_down[0].val.clusterDim.x = M.split;
+    cfg_down.gridDim = dim3(runs * M.split);
+    cfg_down.numAttrs = 2;
+    cfg_down.dynamicSmemBytes = smem_down;
+    return cudaLaunchKernelEx(&cfg_down, down_split, d_map, M) == cudaSuccess ? SQNN_OK : SQNN_E_CUDA;
 }
 
 int moe_queue(const sqnn_moe *L, uint32_t tokens, const void *d_x, int x_dtype, int64_t ldx, void *d_y, int y_dtype, int64_t ldy,

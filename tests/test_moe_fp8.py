@@ -102,6 +102,17 @@ def test_larger(tokens, experts, top_k, hidden, inner, x_type):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("tokens,experts,top_k,hidden,inner,x_type", [
+    (29, 8, 7, 367, 3264, F32), (2, 64, 8, 384, 2864, BF16), (3, 20, 4, 690, 1500, BF16), (5, 16, 6, 700, 2000, F32), (9, 12, 3, 1100, 2000, BF16),
+    (64, 8, 4, 500, 3000, F32), (1, 9, 9, 17, 700, BF16)])
+def test_rows_shared_by_a_cluster(tokens, experts, top_k, hidden, inner, x_type):
+    lay, x = layer(experts, hidden, inner, x_type, tokens + inner), tokens_of(tokens, hidden, x_type, 10)
+    first = call(x, lay, top_k)
+    check(x, lay, top_k, first)
+    assert all(torch.equal(a, b) for a, b in zip(call(x, lay, top_k), first))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,experts,top_k,hidden,inner,x_type", [
     (64, 8, 2, 3200, 400, BF16), (64, 8, 2, 4096, 384, F32), (20, 16, 3, 3300, 256, BF16), (25, 6, 6, 5000, 130, BF16),     # many tokens, wide outputs
     (32, 512, 16, 256, 128, BF16), (64, 256, 1, 128, 64, F32), (2, 512, 16, 300, 100, F32),                                # most experts, most logits
     (1, 2, 1, 11264, 300, F32), (3, 4, 2, 11264, 129, BF16), (5, 2, 2, 11264, 11264, F32), (64, 3, 3, 300, 11264, BF16)])  # widest
@@ -219,7 +230,7 @@ def test_own_stream_graph_and_two_at_once():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("tokens,experts,hidden,inner", [(1, 4, 512, 256), (20, 8, 3500, 700)])
+@pytest.mark.parametrize("tokens,experts,hidden,inner", [(1, 4, 512, 256), (20, 8, 3500, 700), (3, 16, 400, 2500)])
 def test_a_wait_that_gives_up_ends_the_call(tokens, experts, hidden, inner):
     lay, x = layer(experts, hidden, inner, F32, 21), tokens_of(tokens, hidden, F32, 22)
     good = call(x, lay, 2)
