@@ -314,57 +314,90 @@ SQNN_DEV void logits_of_cluster(const MoeArgs &M, int64_t *keys, double *scratch
     }
 }
 
-// fp32: a warp per expert, four tokens and a share of the columns; eight products at a time.
-SQNN_DEV void logits_of_cluster(const MoeArgs &M, int64_t *keys, double *scratch, Routing &R, const float *x, const float *router)
+// fp32: a warp has OWN experts, four tokens and a share of the columns; eight products at a time.  OWN is four where there are enough of them: each row of x
+// and of the router comes from L2 (the SM's memory is all taken; 18 tokens, 7 of 128 experts, 1200 x 128: 97 us for the call with one, 64 with four).
+template <uint32_t OWN, bool VEC>
+SQNN_DEV void logits_by(const MoeArgs &M, int64_t *keys, double *scratch, Routing &R, const float *x, const float *router)
 {
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank();
-    constexpr uint32_t SHARE = 4;                                // tokens that share a read of an expert's row
-    const uint32_t mine = (M.experts - rank + CLUSTER - 1) / CLUSTER, groups = (M.tokens + SHARE - 1) / SHARE, tasks = max(mine, 1u) * groups;
+    constexpr uint32_t SHARE = 4, SUMS = OWN * SHARE;            // SHARE: tokens that share a read of an expert's row
+    const uint32_t mine = (M.experts - rank + CLUSTER - 1) / CLUSTER, groups = (M.tokens + SHARE - 1) / SHARE, tasks = (max(mine, 1u) + OWN - 1) / OWN * groups;
     const uint32_t parts = tasks < WARPS ? WARPS / tasks : 1, steps = (M.hidden + 255) / 256;
+    // this lane's eight of 256 columns: neighbours, or (rows off 16-byte boundaries) every 32nd
+    auto values = [&](const float *row, uint32_t c, float (&v)[8]) {
+        if constexpr (VEC) {
+            row_values8(row, c * 256 + lane * 8, M.hidden, true, v);
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) {
+                const uint32_t at = c * 256 + j * 32 + lane;
+                v[j] = at < M.hidden ? row[at] : 0.0f;
+            }
+        }
+    };
     if (parts == 1) cluster_wait();
 #pragma unroll 1
     for (uint32_t i = warp; i < tasks * parts; i += WARPS) {
-        const uint32_t task = i / parts, part = i - task * parts, own = task / groups, t0 = task % groups * SHARE;
-        const float *const r_row = router + (int64_t)min(rank + CLUSTER * own, M.experts - 1) * M.ldr;
-        double sum[SHARE] = {};
+        const uint32_t task = i / parts, part = i - task * parts, own = task / groups * OWN, t0 = task % groups * SHARE;
+        double sum[SUMS] = {};
         uint32_t top[SHARE] = {};
-#pragma unroll 2
+#pragma unroll (OWN == 1 ? 2 : 1)
         for (uint32_t c = steps * part / parts; c < steps * (part + 1) / parts; ++c) {
-            const uint32_t at = c * 256 + lane * 8;
-            float r[8];
-            row_values8(r_row, at, M.hidden, M.r_vec, r);
+            float r[OWN][8];
+#pragma unroll
+            for (uint32_t o = 0; o < OWN; ++o) values(router + (int64_t)min(rank + CLUSTER * (own + o), M.experts - 1) * M.ldr, c, r[o]);
 #pragma unroll
             for (uint32_t t = 0; t < SHARE; ++t) {
-                float v[8], s = 0.0f;
-                row_values8(x + (int64_t)min(t0 + t, M.tokens - 1) * M.ldx, at, M.hidden, M.x_vec, v);
+                float v[8];
+                values(x + (int64_t)min(t0 + t, M.tokens - 1) * M.ldx, c, v);
 #pragma unroll
-                for (uint32_t j = 0; j < 8; ++j) {
-                    s = fmaf(r[j], v[j], s);
-                    top[t] = max(top[t], __float_as_uint(v[j]) & 0x7fffffffu);
+                for (uint32_t j = 0; j < 8; ++j) top[t] = max(top[t], __float_as_uint(v[j]) & 0x7fffffffu);
+#pragma unroll
+                for (uint32_t o = 0; o < OWN; ++o) {
+                    float s = 0.0f;
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) s = fmaf(r[o][j], v[j], s);
+                    sum[o * SHARE + t] += (double)s;
                 }
-                sum[t] += (double)s;
             }
         }
 #pragma unroll
-        for (uint32_t t = 0; t < SHARE; ++t) {
+        for (uint32_t k = 0; k < SUMS; ++k)
 #pragma unroll
-            for (uint32_t d = 16; d; d >>= 1) sum[t] += __shfl_xor_sync(0xffffffffu, sum[t], d);
+            for (uint32_t d = 16; d; d >>= 1) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], d);
+#pragma unroll
+        for (uint32_t t = 0; t < SHARE; ++t) {
             const uint32_t most = __reduce_max_sync(0xffffffffu, top[t]);
             if (lane == 0 && t0 + t < M.tokens) {
                 if (own == 0) atomicMax(&R.largest[t0 + t], most);
-                if (parts > 1) scratch[i * SHARE + t] = sum[t];
-                else if (own < mine) send_logit(M, keys, t0 + t, rank + CLUSTER * own, sum[t]);
+#pragma unroll
+                for (uint32_t o = 0; o < OWN; ++o) {
+                    if (parts > 1) scratch[i * SUMS + o * SHARE + t] = sum[o * SHARE + t];
+                    else if (own + o < mine) send_logit(M, keys, t0 + t, rank + CLUSTER * (own + o), sum[o * SHARE + t]);
+                }
             }
         }
     }
     if (parts == 1) return;
     __syncthreads();
     cluster_wait();
-    if (tid < tasks * SHARE) {
-        const uint32_t task = tid / SHARE, t = task % groups * SHARE + tid % SHARE;
+    if (tid < tasks * SUMS) {
+        const uint32_t task = tid / SUMS, k = tid % SUMS, t = task % groups * SHARE + k % SHARE, e = task / groups * OWN + k / SHARE;
+        if (t >= M.tokens || e >= mine) return;
         double sum = 0.0;
-        for (uint32_t p = 0; p < parts; ++p) sum += scratch[(task * parts + p) * SHARE + tid % SHARE];
-        if (t < M.tokens && task / groups < mine) send_logit(M, keys, t, rank + CLUSTER * (task / groups), sum);
+        for (uint32_t p = 0; p < parts; ++p) sum += scratch[(task * parts + p) * SUMS + k];
+        send_logit(M, keys, t, rank + CLUSTER * e, sum);
+    }
+}
+SQNN_DEV void logits_of_cluster(const MoeArgs &M, int64_t *keys, double *scratch, Routing &R, const float *x, const float *router)
+{
+    const bool few = (M.experts + CLUSTER - 1) / CLUSTER * ((M.tokens + 3) / 4) <= 2 * WARPS;
+    if (M.x_vec && M.r_vec) {
+        if (few) logits_by<1, true>(M, keys, scratch, R, x, router);
+        else logits_by<4, true>(M, keys, scratch, R, x, router);
+    } else {
+        if (few) logits_by<1, false>(M, keys, scratch, R, x, router);
+        else logits_by<4, false>(M, keys, scratch, R, x, router);
     }
 }
 
