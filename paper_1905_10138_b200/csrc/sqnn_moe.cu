@@ -519,6 +519,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
     for (uint32_t i = tid; i < 2 * M.experts; i += THREADS) (&R.mask[0][0])[i] = 0;
     if (tid == 0) asm volatile("prefetch.tensormap [%0];\n" :: "l"(&weights) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    __syncthreads();                                             // the zeros are there before any warp adds a maximum
     wait_prior_grid();
     launch_dependents();
     cluster_arrive();
