@@ -450,6 +450,7 @@ SQNN_DEV void choose(const MoeArgs &M, int64_t *keys, int64_t *chosen, Routing &
         for (uint32_t d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         if (lane == 0) R.total[t] = sum;
     }
+    fence_async_smem();                                          // the rings' copies come after all that was written where they go, here last
     __syncthreads();
     static_assert(MAX_EXPERTS <= THREADS, "an expert per thread");
     const uint32_t groups = tid < M.experts ? (tokens_of(R, tid) + M.per - 1) / M.per : 0;
@@ -553,7 +554,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
         }
     };
     if constexpr (EARLY) stage(0, M.tokens, ALL, 0);
-    fence_async_smem();                                          // the rings' copies come after what was written there
     choose(M, keys, reinterpret_cast<int64_t *>(parts), R);
     if (blockIdx.x == 0) {                                       // for the caller and for the second kernel
         for (uint32_t i = tid; i < M.tokens * M.top_k; i += THREADS) {

@@ -21,3 +21,14 @@ def test_the_largest_activation_in_one_place(tokens, experts, top_k, hidden, inn
         check(x, lay, top_k, got)
         for _ in range(5):
             assert all(torch.equal(a, b) for a, b in zip(call(x, lay, top_k), got))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,experts,top_k,hidden,inner,x_type", [(64, 256, 16, 256, 64, BF16), (32, 512, 16, 192, 48, F32), (1, 512, 16, 128, 32, BF16)])
+def test_weights_come_after_the_choice(tokens, experts, top_k, hidden, inner, x_type):
+    """The weights' copies go where the logits were, which the choice of experts writes to until it is made: many logits and the most choices, call after call."""
+    lay, x = layer(experts, hidden, inner, x_type, 41), tokens_of(tokens, hidden, x_type, 42)
+    first = call(x, lay, top_k)
+    check(x, lay, top_k, first)
+    for _ in range(20):
+        assert all(torch.equal(a, b) for a, b in zip(call(x, lay, top_k), first))
