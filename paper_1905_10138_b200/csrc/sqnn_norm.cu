@@ -334,7 +334,8 @@ __global__ void __launch_bounds__(MOST, MOST == 384 ? 3 : SLOTS == 1 || (SLOTS =
                 }
                 const uint2 all_hi = make_uint2(hi[0] | (hi[1] << 16), hi[2] | (hi[3] << 16));
                 uint2 all = make_uint2(lo[0] | (lo[1] << 16), lo[2] | (lo[3] << 16));
-                if (all.x != all_hi.x || all.y != all_hi.y)
+                // (c is no fp32 number in rows below 2^-129 whose group is zero, or nearly)
+                if (all.x != all_hi.x || all.y != all_hi.y || c_hi > 0x1.fffffep127f)
                     all = convert_exactly(make_float4(a[0], a[1], a[2], a[3]), make_float4(a[4], a[5], a[6], a[7]), make_float4(w[0], w[1], w[2], w[3]),
                                           make_float4(w[4], w[5], w[6], w[7]), scale_h, rest / (double)s);
                 if (in) {
