@@ -49,5 +49,10 @@ SQNN_DEV void peer_store(uint32_t a, int64_t v)
 {
     asm volatile("st.shared::cluster.s64 [%0], %1;\n" :: "r"(a), "l"(v) : "memory");
 }
+// The larger of what is there and v.
+SQNN_DEV void peer_max(uint32_t a, uint32_t v)
+{
+    asm volatile("red.relaxed.cluster.shared::cluster.max.u32 [%0], %1;\n" :: "r"(a), "r"(v) : "memory");
+}
 
 }  // namespace sqnn

@@ -96,6 +96,7 @@ struct Routing {
     uint32_t totals[WARPS];
     uint32_t entries;
     uint32_t largest[MAX_TOKENS];         // magnitude of a token's largest activation, as bits
+    uint32_t spread[MAX_TOKENS];          // the largest sum of magnitudes of products among a token's logits, or more: fp32 as bits
     float total[MAX_TOKENS];              // what its shares are divided by
 };
 constexpr uint32_t ROUTING_BYTES = (sizeof(Routing) + 127) / 128 * 128;
@@ -182,9 +183,20 @@ SQNN_DEV void weights_of(uint32_t (&a)[4], uint32_t top, uint32_t bottom)
 
 // ---- routing
 
-// Logits of this CTA's experts (every CLUSTER-th), as keys, into the shared memory of all CTAs of the cluster, and the tokens' largest
-// activations.  Waits for the cluster before it writes to others.  Some products at a time are summed in fp32, these sums in 64 bits: which experts a token goes to must not hang on the order of a sum.
-// `scratch`: 16 KB.
+// Logits of this CTA's experts (every CLUSTER-th), as keys, and how far off they may be, into the shared memory of all CTAs of the cluster, and the tokens'
+// largest activations.  Waits for the cluster before it writes to others.
+//
+// Which experts a token goes to must not hang on the order of a sum.  Few logits are near one another, so all are summed in fp32 over a few products at a time (and
+// these sums in 64 bits), beside them the magnitudes of the products, and choose() computes those once more in 64 bits that lie within the error of a chosen
+// one.  (All products in 64 bits: 16 000 cycles of an SM's 64-bit units for 16 tokens and 64 experts of 4096 columns, where this takes 11 600.)  With A the sum of
+// magnitudes:
+//   - bf16: an MMA adds 16 exact products, each cut off below 2^-25 of the largest (as measured), and cuts the sum to 24 bits: at most 5 2^-23 of their magnitudes.  Two
+//     additions of such sums, 2^-24 each, make one of 64 columns: 6 2^-23 A.  A itself comes from such MMAs, at most 2^-11 A too small.
+//   - fp32: eight fused multiply-adds, 2^-24 each: 8 2^-24 A; A at most 2^-17 A too small.
+//   - what lies below 2^-126 may be lost: 2^-125 for each column.  Where a sum passes fp32's range nothing is known.
+// `scratch`: 24 KB.
+template <typename XT> constexpr float SLACK = sizeof(XT) == 2 ? 0x1.81p-21f : 0x1.01p-21f;
+constexpr uint32_t INFINITE = 0x7f800000u, UNKNOWN = 0x7f000000u;         // (2^127: a logit that has passed the range has an A above that)
 // 64-bit floating numbers as integers of the same order; NaN comes last.  And back.
 SQNN_DEV int64_t key_of(double v)
 {
@@ -193,12 +205,28 @@ SQNN_DEV int64_t key_of(double v)
     return b ^ ((b >> 63) & 0x7fffffffffffffffll);
 }
 SQNN_DEV double value_of(int64_t k) { return __longlong_as_double(k ^ ((k >> 63) & 0x7fffffffffffffffll)); }
-SQNN_DEV void send_logit(const MoeArgs &M, int64_t *keys, uint32_t token, uint32_t expert, double v)
+SQNN_DEV void send_logit(int64_t *keys, uint32_t experts, uint32_t token, uint32_t expert, double v)
 {
-    const uint32_t at = smem_addr(keys + token * M.experts + expert);
+    const uint32_t at = smem_addr(keys + token * experts + expert);
     const int64_t key = key_of(v);
 #pragma unroll
     for (uint32_t r = 0; r < CLUSTER; ++r) peer_store(peer_addr(at, r), key);
+}
+SQNN_DEV void send_spread(Routing &R, uint32_t token, uint32_t bits)     // (NaN is larger than infinity)
+{
+    const uint32_t at = smem_addr(R.spread + token);
+#pragma unroll
+    for (uint32_t r = 0; r < CLUSTER; ++r) peer_max(peer_addr(at, r), bits);
+}
+SQNN_DEV void mma_bf16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)     // c = a b
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};\n"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+SQNN_DEV void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
 // 16 bf16 numbers of a row from `at` on, zero from `n` on.  (What is seldom run is kept out of line, here and below: the kernels run once
@@ -216,34 +244,23 @@ static __device__ __noinline__ float4 ragged4(const float *row, uint32_t at, uin
 {
     return make_float4(at < n ? row[at] : 0.0f, at + 1 < n ? row[at + 1] : 0.0f, at + 2 < n ? row[at + 2] : 0.0f, at + 3 < n ? row[at + 3] : 0.0f);
 }
-SQNN_DEV void raw16(const __nv_bfloat16 *row, uint32_t at, uint32_t n, bool vec, uint32_t (&v)[8])
+SQNN_DEV void load16(const __nv_bfloat16 *p, uint32_t (&v)[8])
 {
-    uint4 a = make_uint4(0, 0, 0, 0), b = a;
-    if (vec && at + 16 <= n) {
-        a = *reinterpret_cast<const uint4 *>(row + at);
-        b = *reinterpret_cast<const uint4 *>(row + at + 8);
-    } else if (at < n) {
-        a = ragged8(row, at, n);
-        b = ragged8(row, at + 8, n);
-    }
+    const uint4 a = *reinterpret_cast<const uint4 *>(p), b = *reinterpret_cast<const uint4 *>(p + 8);
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
-
-SQNN_DEV void row_values8(const float *row, uint32_t at, uint32_t n, bool vec, float (&v)[8])
+SQNN_DEV void ragged16(const __nv_bfloat16 *row, uint32_t at, uint32_t n, uint32_t (&v)[8])
 {
-    float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
-    if (vec && at + 8 <= n) {
-        a = *reinterpret_cast<const float4 *>(row + at);
-        b = *reinterpret_cast<const float4 *>(row + at + 4);
-    } else if (at < n) {
-        a = ragged4(row, at, n);
-        b = ragged4(row, at + 4, n);
-    }
+    const uint4 a = ragged8(row, at, n), b = ragged8(row, at + 8, n);
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
-SQNN_DEV void row_values8(const __nv_bfloat16 *row, uint32_t at, uint32_t n, bool vec, float (&v)[8])
+SQNN_DEV void load8(const float *p, float (&v)[8])
 {
-    const uint4 f = vec && at + 8 <= n ? *reinterpret_cast<const uint4 *>(row + at) : at < n ? ragged8(row, at, n) : make_uint4(0, 0, 0, 0);
+    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+SQNN_DEV void unpack8(const uint4 &f, float (&v)[8])
+{
     const uint32_t u[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
@@ -251,8 +268,26 @@ SQNN_DEV void row_values8(const __nv_bfloat16 *row, uint32_t at, uint32_t n, boo
         v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
     }
 }
+SQNN_DEV void load8(const __nv_bfloat16 *p, float (&v)[8]) { unpack8(*reinterpret_cast<const uint4 *>(p), v); }
+SQNN_DEV void row_values8(const float *row, uint32_t at, uint32_t n, bool vec, float (&v)[8])
+{
+    if (vec && at + 8 <= n) {
+        load8(row + at, v);
+    } else {
+        float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
+        if (at < n) {
+            a = ragged4(row, at, n);
+            b = ragged4(row, at + 4, n);
+        }
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+}
+SQNN_DEV void row_values8(const __nv_bfloat16 *row, uint32_t at, uint32_t n, bool vec, float (&v)[8])
+{
+    unpack8(vec && at + 8 <= n ? *reinterpret_cast<const uint4 *>(row + at) : at < n ? ragged8(row, at, n) : make_uint4(0, 0, 0, 0), v);
+}
 
-// bf16: on the tensor cores, 16 experts by 8 tokens by 64 columns (four MMAs, products exact) at a time.  The columns of a tile are shared by as
+// bf16: on the tensor cores, 16 experts by 8 tokens by 64 columns (four MMAs of their own, products exact) at a time.  The columns of a tile are shared by as
 // many warps as there are to spare.
 SQNN_DEV void logits_of_cluster(const MoeArgs &M, int64_t *keys, double *scratch, Routing &R, const __nv_bfloat16 *x, const __nv_bfloat16 *router)
 {
@@ -260,6 +295,8 @@ SQNN_DEV void logits_of_cluster(const MoeArgs &M, int64_t *keys, double *scratch
     // (a CTA without experts still looks at the tokens)
     const uint32_t mine = (M.experts - rank + CLUSTER - 1) / CLUSTER, n_tiles = (M.tokens + 7) / 8, tiles = (max(mine, 1u) + 15) / 16 * n_tiles;
     const uint32_t parts = tiles < WARPS ? WARPS / tiles : 1, steps = (M.hidden + 63) / 64;
+    float *const totals = reinterpret_cast<float *>(scratch + WARPS * 128);
+    const bool vec = M.x_vec && M.r_vec;
     if (parts == 1) cluster_wait();
 #pragma unroll 1
     for (uint32_t i = warp; i < tiles * parts; i += WARPS) {
@@ -268,24 +305,39 @@ SQNN_DEV void logits_of_cluster(const MoeArgs &M, int64_t *keys, double *scratch
         const __nv_bfloat16 *const rb = router + (int64_t)min(rank + CLUSTER * (e0 + g + 8), M.experts - 1) * M.ldr;
         const __nv_bfloat16 *const xr = x + (int64_t)min(t0 + g, M.tokens - 1) * M.ldx;
         double sum[4] = {};
-        uint32_t top = 0;
-#pragma unroll 2
-        for (uint32_t c = steps * part / parts; c < steps * (part + 1) / parts; ++c) {
+        float total[4] = {};                                     // of magnitudes
+        uint32_t top = 0, na[8], nb[8], nv[8];
+        auto ask = [&](uint32_t c) {                             // (one test for all, so that all are under way together)
             const uint32_t at = c * 64 + t4 * 16;
+            if (vec && at + 16 <= M.hidden) {
+                load16(ra + at, na);
+                load16(rb + at, nb);
+                load16(xr + at, nv);
+            } else {
+                ragged16(ra, at, M.hidden, na);
+                ragged16(rb, at, M.hidden, nb);
+                ragged16(xr, at, M.hidden, nv);
+            }
+        };
+        const uint32_t c0 = steps * part / parts, c1 = steps * (part + 1) / parts;
+        ask(c0);                                                 // (more parts than steps: columns of another's, or zeros, that nobody looks at)
+#pragma unroll 1
+        for (uint32_t c = c0; c < c1; ++c) {
             uint32_t a[8], b[8], v[8];
-            raw16(ra, at, M.hidden, M.r_vec, a);
-            raw16(rb, at, M.hidden, M.r_vec, b);
-            raw16(xr, at, M.hidden, M.x_vec, v);
-            float s[4] = {};
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) { a[j] = na[j]; b[j] = nb[j]; v[j] = nv[j]; }
+            if (c + 1 < c1) ask(c + 1);
+            float s[4][4];
+            constexpr uint32_t MAGNITUDE = 0x7fff7fffu;
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) {
-                asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
-                             : "+f"(s[0]), "+f"(s[1]), "+f"(s[2]), "+f"(s[3])
-                             : "r"(a[2 * j]), "r"(b[2 * j]), "r"(a[2 * j + 1]), "r"(b[2 * j + 1]), "r"(v[2 * j]), "r"(v[2 * j + 1]));
-                top = __vmaxu2(top, __vmaxu2(v[2 * j] & 0x7fff7fffu, v[2 * j + 1] & 0x7fff7fffu));
+                const uint32_t x0 = v[2 * j] & MAGNITUDE, x1 = v[2 * j + 1] & MAGNITUDE;
+                mma_bf16_first(s[j], a[2 * j], b[2 * j], a[2 * j + 1], b[2 * j + 1], v[2 * j], v[2 * j + 1]);
+                mma_bf16(total, a[2 * j] & MAGNITUDE, b[2 * j] & MAGNITUDE, a[2 * j + 1] & MAGNITUDE, b[2 * j + 1] & MAGNITUDE, x0, x1);
+                top = __vmaxu2(top, __vmaxu2(x0, x1));
             }
 #pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) sum[j] += (double)s[j];
+            for (uint32_t j = 0; j < 4; ++j) sum[j] += (double)((s[0][j] + s[1][j]) + (s[2][j] + s[3][j]));
         }
         if (e0 == 0) {
             top = max(top & 0xffffu, top >> 16) << 16;
@@ -297,7 +349,16 @@ SQNN_DEV void logits_of_cluster(const MoeArgs &M, int64_t *keys, double *scratch
         for (uint32_t j = 0; j < 4; ++j) {
             const uint32_t e = e0 + g + (j >> 1) * 8, t = t0 + 2 * t4 + (j & 1);
             if (parts > 1) scratch[i * 128 + j * 32 + lane] = sum[j];
-            else if (e < mine && t < M.tokens) send_logit(M, keys, t, rank + CLUSTER * e, sum[j]);
+            else if (e < mine && t < M.tokens) send_logit(keys, M.experts, t, rank + CLUSTER * e, sum[j]);
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {                       // the largest of 16 experts
+            uint32_t most = max(__float_as_uint(total[k]), __float_as_uint(total[2 + k]));      // (experts past the last repeat it)
+#pragma unroll
+            for (uint32_t d = 4; d < 32; d <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
+            const uint32_t t = 2 * t4 + k;
+            if (g == 0 && parts > 1) totals[i * 8 + t] = __uint_as_float(most);
+            else if (g == 0 && t0 + t < M.tokens) send_spread(R, t0 + t, most);
         }
     }
     if (parts == 1) return;
@@ -310,48 +371,89 @@ SQNN_DEV void logits_of_cluster(const MoeArgs &M, int64_t *keys, double *scratch
         for (uint32_t p = i4 & 3; p < parts; p += 4) sum += scratch[(tile * parts + p) * 128 + (i & 127)];
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        if ((i4 & 3) == 0 && e < mine && t < M.tokens) send_logit(M, keys, t, rank + CLUSTER * e, sum);
+        if ((i4 & 3) == 0 && e < mine && t < M.tokens) send_logit(keys, M.experts, t, rank + CLUSTER * e, sum);
+    }
+    const uint32_t item = tid / 4 - THREADS / 8;                 // a token's parts in a tile, by the largest expert of each; four threads
+    if (item < tiles * 8) {
+        const uint32_t tile = item / 8, t = tile % n_tiles * 8 + item % 8;
+        float total = 0.0f;
+        for (uint32_t p = tid & 3; p < parts; p += 4) total += totals[(tile * parts + p) * 8 + item % 8];
+        total += __shfl_xor_sync(0xffffffffu, total, 1);
+        total += __shfl_xor_sync(0xffffffffu, total, 2);
+        if ((tid & 3) == 0 && t < M.tokens) send_spread(R, t, __float_as_uint(total));
     }
 }
 
 // fp32: a warp has OWN experts, four tokens and a share of the columns; eight products at a time.  OWN is four where there are enough of them: each row of x
-// and of the router comes from L2 (the SM's memory is all taken; 18 tokens, 7 of 128 experts, 1200 x 128: 97 us for the call with one, 64 with four).
+// and of the router comes from L2 (the SM's memory is all taken; 18 tokens, 7 of 128 experts, 1200 x 128: 97 us for the call with one, 64 with four).  Functions of their
+// own, so that the registers they need are not missing elsewhere.
 template <uint32_t OWN, bool VEC>
-SQNN_DEV void logits_by(const MoeArgs &M, int64_t *keys, double *scratch, Routing &R, const float *x, const float *router)
+static __device__ __noinline__ void logits_by(uint32_t tokens, uint32_t experts, uint32_t hidden, const float *x, int64_t ldx, const float *router, int64_t ldr, int64_t *keys,
+                                              double *scratch, Routing &R)
 {
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank();
     constexpr uint32_t SHARE = 4, SUMS = OWN * SHARE;            // SHARE: tokens that share a read of an expert's row
-    const uint32_t mine = (M.experts - rank + CLUSTER - 1) / CLUSTER, groups = (M.tokens + SHARE - 1) / SHARE, tasks = (max(mine, 1u) + OWN - 1) / OWN * groups;
-    const uint32_t parts = tasks < WARPS ? WARPS / tasks : 1, steps = (M.hidden + 255) / 256;
+    const uint32_t mine = (experts - rank + CLUSTER - 1) / CLUSTER, groups = (tokens + SHARE - 1) / SHARE, tasks = (max(mine, 1u) + OWN - 1) / OWN * groups;
+    const uint32_t parts = tasks < WARPS ? WARPS / tasks : 1, steps = (hidden + 255) / 256;
     // this lane's eight of 256 columns: neighbours, or (rows off 16-byte boundaries) every 32nd
     auto values = [&](const float *row, uint32_t c, float (&v)[8]) {
         if constexpr (VEC) {
-            row_values8(row, c * 256 + lane * 8, M.hidden, true, v);
+            row_values8(row, c * 256 + lane * 8, hidden, true, v);
         } else {
 #pragma unroll
             for (uint32_t j = 0; j < 8; ++j) {
                 const uint32_t at = c * 256 + j * 32 + lane;
-                v[j] = at < M.hidden ? row[at] : 0.0f;
+                v[j] = at < hidden ? row[at] : 0.0f;
             }
         }
     };
+    const auto expert_row = [&](uint32_t e) { return router + (int64_t)min(rank + CLUSTER * e, experts - 1) * ldr; };
+    const auto token_row = [&](uint32_t t) { return x + (int64_t)min(t, tokens - 1) * ldx; };
+    constexpr bool AT_ONCE = OWN == 1 && VEC;                    // the rows of x too (where registers allow)
+    float *const totals = reinterpret_cast<float *>(scratch + WARPS * SUMS);
     if (parts == 1) cluster_wait();
 #pragma unroll 1
     for (uint32_t i = warp; i < tasks * parts; i += WARPS) {
         const uint32_t task = i / parts, part = i - task * parts, own = task / groups * OWN, t0 = task % groups * SHARE;
         double sum[SUMS] = {};
+        float total[SHARE] = {};                                 // of magnitudes, or more: the largest of eight of x times the largest expert's eight of the router
         uint32_t top[SHARE] = {};
-#pragma unroll (OWN == 1 ? 2 : 1)
+#pragma unroll (OWN == 1 && !VEC ? 2 : 1)
         for (uint32_t c = steps * part / parts; c < steps * (part + 1) / parts; ++c) {
-            float r[OWN][8];
+            float r[OWN][8], rows[AT_ONCE ? SHARE : 1][8];
+            if (VEC && c * 256 + lane * 8 + 8 <= hidden) {       // (one test for all, so that all are under way together)
 #pragma unroll
-            for (uint32_t o = 0; o < OWN; ++o) values(router + (int64_t)min(rank + CLUSTER * (own + o), M.experts - 1) * M.ldr, c, r[o]);
+                for (uint32_t o = 0; o < OWN; ++o) load8(expert_row(own + o) + c * 256 + lane * 8, r[o]);
+#pragma unroll
+                for (uint32_t t = 0; AT_ONCE && t < SHARE; ++t) load8(token_row(t0 + t) + c * 256 + lane * 8, rows[t]);
+            } else {
+#pragma unroll
+                for (uint32_t o = 0; o < OWN; ++o) values(expert_row(own + o), c, r[o]);
+#pragma unroll
+                for (uint32_t t = 0; AT_ONCE && t < SHARE; ++t) values(token_row(t0 + t), c, rows[t]);
+            }
+            float eight = 0.0f;
+#pragma unroll
+            for (uint32_t o = 0; o < OWN; ++o) {
+                float s = 0.0f;
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) s += fabsf(r[o][j]);
+                eight = fmaxf(eight, s);                         // (NaN is seen in its logit)
+            }
 #pragma unroll
             for (uint32_t t = 0; t < SHARE; ++t) {
                 float v[8];
-                values(x + (int64_t)min(t0 + t, M.tokens - 1) * M.ldx, c, v);
+                if constexpr (AT_ONCE) {
 #pragma unroll
-                for (uint32_t j = 0; j < 8; ++j) top[t] = max(top[t], __float_as_uint(v[j]) & 0x7fffffffu);
+                    for (uint32_t j = 0; j < 8; ++j) v[j] = rows[t][j];
+                } else {
+                    values(token_row(t0 + t), c, v);
+                }
+                uint32_t most = 0;
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[j]) & 0x7fffffffu);
+                top[t] = max(top[t], most);
+                total[t] = fmaf(eight, __uint_as_float(most), total[t]);
 #pragma unroll
                 for (uint32_t o = 0; o < OWN; ++o) {
                     float s = 0.0f;
@@ -368,12 +470,16 @@ SQNN_DEV void logits_by(const MoeArgs &M, int64_t *keys, double *scratch, Routin
 #pragma unroll
         for (uint32_t t = 0; t < SHARE; ++t) {
             const uint32_t most = __reduce_max_sync(0xffffffffu, top[t]);
-            if (lane == 0 && t0 + t < M.tokens) {
+#pragma unroll
+            for (uint32_t d = 16; d; d >>= 1) total[t] += __shfl_xor_sync(0xffffffffu, total[t], d);
+            if (lane == 0 && t0 + t < tokens) {
                 if (own == 0) atomicMax(&R.largest[t0 + t], most);
+                if (parts > 1) totals[i * SHARE + t] = total[t];
+                else send_spread(R, t0 + t, __float_as_uint(total[t]));
 #pragma unroll
                 for (uint32_t o = 0; o < OWN; ++o) {
                     if (parts > 1) scratch[i * SUMS + o * SHARE + t] = sum[o * SHARE + t];
-                    else if (own + o < mine) send_logit(M, keys, t0 + t, rank + CLUSTER * (own + o), sum[o * SHARE + t]);
+                    else if (own + o < mine) send_logit(keys, experts, t0 + t, rank + CLUSTER * (own + o), sum[o * SHARE + t]);
                 }
             }
         }
@@ -383,63 +489,129 @@ SQNN_DEV void logits_by(const MoeArgs &M, int64_t *keys, double *scratch, Routin
     cluster_wait();
     if (tid < tasks * SUMS) {
         const uint32_t task = tid / SUMS, k = tid % SUMS, t = task % groups * SHARE + k % SHARE, e = task / groups * OWN + k / SHARE;
-        if (t >= M.tokens || e >= mine) return;
-        double sum = 0.0;
-        for (uint32_t p = 0; p < parts; ++p) sum += scratch[(task * parts + p) * SUMS + k];
-        send_logit(M, keys, t, rank + CLUSTER * e, sum);
+        if (t < tokens && e < mine) {
+            double sum = 0.0;
+            float total = 0.0f;
+            for (uint32_t p = 0; p < parts; ++p) {
+                sum += scratch[(task * parts + p) * SUMS + k];
+                total += totals[(task * parts + p) * SHARE + k % SHARE];
+            }
+            send_logit(keys, experts, t, rank + CLUSTER * e, sum);
+            if (k < SHARE) send_spread(R, t, __float_as_uint(total));
+        }
     }
 }
 SQNN_DEV void logits_of_cluster(const MoeArgs &M, int64_t *keys, double *scratch, Routing &R, const float *x, const float *router)
 {
     const bool few = (M.experts + CLUSTER - 1) / CLUSTER * ((M.tokens + 3) / 4) <= 2 * WARPS;
     if (M.x_vec && M.r_vec) {
-        if (few) logits_by<1, true>(M, keys, scratch, R, x, router);
-        else logits_by<4, true>(M, keys, scratch, R, x, router);
+        if (few) logits_by<1, true>(M.tokens, M.experts, M.hidden, x, M.ldx, router, M.ldr, keys, scratch, R);
+        else logits_by<4, true>(M.tokens, M.experts, M.hidden, x, M.ldx, router, M.ldr, keys, scratch, R);
     } else {
-        if (few) logits_by<1, false>(M, keys, scratch, R, x, router);
-        else logits_by<4, false>(M, keys, scratch, R, x, router);
+        if (few) logits_by<1, false>(M.tokens, M.experts, M.hidden, x, M.ldx, router, M.ldr, keys, scratch, R);
+        else logits_by<4, false>(M.tokens, M.experts, M.hidden, x, M.ldx, router, M.ldr, keys, scratch, R);
+    }
+}
+
+// A token's logits that lie within `slack` of another one among the top_k, once more in 64 bits.  (The last of these counts as near itself: what is near a chosen one
+// from below is near the last, and so is that chosen one.)  All lanes of a warp.
+template <typename XT>
+static __device__ __noinline__ void settle_logits(const XT *x, const XT *router, int64_t ldr, uint32_t hidden, uint32_t experts, uint32_t top_k, bool vec,
+                                                  int64_t *row, const int64_t *best, const int32_t *ids, double slack)
+{
+    const uint32_t lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (uint32_t e0 = 0; e0 < experts; e0 += 32) {
+        const uint32_t e = e0 + lane;
+        bool near = false;
+        if (e < experts) {
+            const double v = value_of(row[e]);
+#pragma unroll 1
+            for (uint32_t s = 0; s < top_k; ++s) near |= (ids[s] != (int32_t)e || s + 1 == top_k) && !(fabs(v - value_of(best[s])) > slack);
+        }
+#pragma unroll 1
+        for (uint32_t left = __ballot_sync(0xffffffffu, near); left; left &= left - 1) {
+            const uint32_t n = e0 + (uint32_t)__ffs((int)left) - 1;
+            const XT *const r = router + (int64_t)n * ldr;
+            double sum = 0.0;
+            if (vec) {
+#pragma unroll 4
+                for (uint32_t at = lane * 8; at + 8 <= hidden; at += 256) {
+                    float a[8], b[8];
+                    load8(x + at, a);
+                    load8(r + at, b);
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) sum = fma((double)a[j], (double)b[j], sum);
+                }
+            }
+#pragma unroll 4
+            for (uint32_t at = (vec ? hidden & ~7u : 0u) + lane; at < hidden; at += 32) sum = fma((double)(float)x[at], (double)(float)r[at], sum);
+#pragma unroll
+            for (uint32_t d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            if (lane == 0) row[n] = key_of(sum);
+        }
+        __syncwarp();
     }
 }
 
 // From logits to the top_k experts of each token, their shares, and the list of (expert, group of up to `per` of its tokens), ascending.  NaN counts as the
 // largest, so that there are always top_k different experts.  All threads; masks are zero before, ends with a barrier.  `chosen`: 8 KB.
+template <typename XT>
 SQNN_DEV void choose(const MoeArgs &M, int64_t *keys, int64_t *chosen, Routing &R)
 {
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // a warp per token: the largest key top_k times, by the upper half, the lower half, the index; the lane that has it notes it down
     for (uint32_t t = warp; t < M.tokens; t += WARPS) {
         int2 *const row = reinterpret_cast<int2 *>(keys + t * M.experts);
-        int2 *const best_of = reinterpret_cast<int2 *>(chosen + t * M.top_k);
+        int64_t *const best = chosen + t * M.top_k;
         int32_t *const ids = R.ids + t * M.top_k;
         constexpr int32_t TAKEN = -0x7fffffff - 1;               // below all keys
+        constexpr int64_t LOWEST = -0x7fffffffffffffffll - 1;    // such a key
 #pragma unroll 1
-        for (uint32_t s = 0; s < M.top_k; ++s) {
-            int2 best = make_int2(0, TAKEN);
-            uint32_t at = MAX_EXPERTS;
-            for (uint32_t e = lane; e < M.experts; e += 32) {
-                const int2 k = row[e];
-                if (k.y > best.y || (k.y == best.y && (uint32_t)k.x > (uint32_t)best.x)) { best = k; at = e; }
+        for (bool settled = false;; settled = true) {
+#pragma unroll 1
+            for (uint32_t s = 0; s < M.top_k; ++s) {
+                int2 top = make_int2(0, TAKEN);
+                uint32_t at = MAX_EXPERTS;
+                for (uint32_t e = lane; e < M.experts; e += 32) {
+                    const int2 k = row[e];
+                    if (k.y > top.y || (k.y == top.y && (uint32_t)k.x > (uint32_t)top.x)) { top = k; at = e; }
+                }
+                const int32_t upper = __reduce_max_sync(0xffffffffu, top.y);
+                bool mine = top.y == upper;
+                const uint32_t who = __ballot_sync(0xffffffffu, mine);
+                if (who & (who - 1)) {
+                    const uint32_t lower = __reduce_max_sync(0xffffffffu, mine ? (uint32_t)top.x : 0u);
+                    mine = mine && (uint32_t)top.x == lower;
+                    const uint32_t lowest = __reduce_min_sync(0xffffffffu, mine ? at : MAX_EXPERTS);     // (by all lanes)
+                    mine = mine && at == lowest;
+                }
+                if (mine) {
+                    *reinterpret_cast<int2 *>(best + s) = top;
+                    ids[s] = (int32_t)at;
+                    row[at] = make_int2(0, TAKEN);
+                }
             }
-            const int32_t upper = __reduce_max_sync(0xffffffffu, best.y);
-            bool mine = best.y == upper;
-            const uint32_t who = __ballot_sync(0xffffffffu, mine);
-            if (who & (who - 1)) {
-                const uint32_t lower = __reduce_max_sync(0xffffffffu, mine ? (uint32_t)best.x : 0u);
-                mine = mine && (uint32_t)best.x == lower;
-                const uint32_t lowest = __reduce_min_sync(0xffffffffu, mine ? at : MAX_EXPERTS);     // (by all lanes)
-                mine = mine && at == lowest;
-            }
-            if (mine) {
-                ids[s] = (int32_t)at;
-                best_of[s] = best;
-                row[at] = make_int2(0, TAKEN);
-            }
+            __syncwarp();
+            // Equal or nearly equal ones among these?  (Logits of zeros are zero; of infinities and NaN nothing better is to be had.)
+            const uint32_t largest = R.largest[t], spread = R.spread[t];
+            if (settled || largest == 0 || largest >= INFINITE) break;
+            const float slack = __uint_as_float(spread < UNKNOWN ? spread : INFINITE) * (2 * SLACK<XT>) + 0x1p-124f * (float)M.hidden;
+            int64_t left = LOWEST;                                    // the largest that is left, lane by lane
+            for (uint32_t e = lane; e < M.experts; e += 32) left = max(left, keys[t * M.experts + e]);
+            const double last = value_of(best[M.top_k - 1]);
+            bool near = left != LOWEST && !(last - value_of(left) > slack);
+            if (lane + 1 < M.top_k) near |= !(value_of(best[lane]) - value_of(best[lane + 1]) > slack);
+            if (!__any_sync(0xffffffffu, near)) break;
+            if (lane < M.top_k) (keys + t * M.experts)[ids[lane]] = best[lane];
+            __syncwarp();
+            settle_logits<XT>(static_cast<const XT *>(M.x) + (int64_t)t * M.ldx, static_cast<const XT *>(M.router), M.ldr, M.hidden, M.experts, M.top_k, M.x_vec && M.r_vec,
+                              keys + t * M.experts, best, ids, slack);
         }
-        __syncwarp();
-        const double first = value_of(chosen[t * M.top_k]);
+        const double first = value_of(best[0]);
         float sum = 0.0f;
         if (lane < M.top_k) {
-            sum = expf((float)(value_of(chosen[t * M.top_k + lane]) - first));
+            sum = expf((float)(value_of(best[lane]) - first));
             R.probs[t * M.top_k + lane] = sum;
             atomicOr(&R.mask[ids[lane]][t >> 5], 1u << (t & 31));
         }
@@ -516,7 +688,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
     const Waits W{&abort_word, M.status, M.wait_limit};
     if (tid < STREAMS * UP_DEPTH) mbar_init(smem_addr(bars + tid), 1);
     if (tid == 0) abort_word = 0;
-    if (tid < MAX_TOKENS) R.largest[tid] = 0;
+    if (tid < MAX_TOKENS) R.largest[tid] = R.spread[tid] = 0;
     for (uint32_t i = tid; i < 2 * M.experts; i += THREADS) (&R.mask[0][0])[i] = 0;
     if (tid == 0) asm volatile("prefetch.tensormap [%0];\n" :: "l"(&weights) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -554,7 +726,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
         }
     };
     if constexpr (EARLY) stage(0, M.tokens, ALL, 0);
-    choose(M, keys, reinterpret_cast<int64_t *>(parts), R);
+    choose<XT>(M, keys, reinterpret_cast<int64_t *>(parts), R);
     if (blockIdx.x == 0) {                                       // for the caller and for the second kernel
         for (uint32_t i = tid; i < M.tokens * M.top_k; i += THREADS) {
             if (M.ids_out) M.ids_out[i] = R.ids[i];
