@@ -841,7 +841,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_moe_up(const __grid_constant__ C
             for (uint32_t d = 4; d < 32; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
             const uint32_t ex = exponent_of(top);
             const float s = scale_of(ex);
-            const uint32_t hi = f16x2(va * s, vb * s), lo = f16x2(va * s - f16_lo(hi), vb * s - f16_hi(hi));
+            // (infinity minus infinity: nothing is left of what has passed fp32's range)
+            const uint32_t hi = f16x2(va * s, vb * s), lo = top == 0x7f800000u ? 0u : f16x2(va * s - f16_lo(hi), vb * s - f16_hi(hi));
             const uint32_t column = 2 * t4 + k;
             if (column < count) {
                 const uint32_t t = token_of(R, e, (en >> 16) * M.per + column);

@@ -32,3 +32,21 @@ def test_weights_come_after_the_choice(tokens, experts, top_k, hidden, inner, x_
     check(x, lay, top_k, first)
     for _ in range(20):
         assert all(torch.equal(a, b) for a, b in zip(call(x, lay, top_k), first))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("x_type", [BF16, F32])
+@pytest.mark.parametrize("hidden,inner", [(520, 96), (2048, 300)])
+def test_inner_values_beyond_fp32_are_infinite(hidden, inner, x_type):
+    """Positive weights throughout: y is infinite, not NaN, where gate and up are finite and their product is not."""
+    router, gu, gus, down, ds = layer(5, hidden, inner, x_type, 51)
+    for w in (gu, down):
+        w.view(torch.uint8).bitwise_and_(0x7f).clamp_(min=8)       # no zeros: 0 x infinity is NaN
+    lay = (router, gu, gus, down, ds)
+    x = tokens_of(4, hidden, x_type, 52).abs()
+    x[1] *= 1e25
+    y, _, probs = call(x, lay, 1)
+    assert bool((probs == 1).all()) and bool((y[1] == float("inf")).all())
+    rest = [0, 2, 3]
+    check(x[rest], lay, 1, call(x[rest], lay, 1))
+    assert all(torch.equal(y[t], v) for t, v in zip(rest, call(x[rest], lay, 1)[0]))
