@@ -13,9 +13,10 @@
 // The 16 columns of an MMA are dealt so that its k slots 2 t, 2 t + 1, 2 t + 8, 2 t + 9 are columns 4 t .. 4 t + 3, and B is stored
 // in the order that gives a lane its share of four MMAs in 32 bytes: position 16 t + 4 j + i of 64 holds column 16 j + 4 t + i.
 //
-// Activations are scaled by a power of two so that the largest lies below 2^15, and cut into fp16 pieces: bf16 numbers are exact in
-// one, fp32 numbers keep 22 bits in two (both down to 2^-40 of the largest).  x is scaled per token, the inner values, whose
-// largest nobody knows before all are there, per token and MMA: a unit of the first kernel is the 16 inner values of one MMA of the second.
+// Activations are scaled by a power of two so that the largest lies between 2^14 and 2^15, and cut into fp16 pieces, which end at 2^-24: bf16 numbers, in one piece,
+// are exact down to 2^-31 of the largest, fp32 numbers, in two, are left with 2^-23 of themselves off, or 2^-39 of the largest (as bf16 numbers are below).  (A
+// third MMA would bring the last bit; the weights have four.)  x is scaled per token, the inner values, whose largest nobody knows before all are there, per token and
+// MMA: a unit of the first kernel is the 16 inner values of one MMA of the second.
 // Sums are fp32 in the MMA, then scaled and added to 32-bit sums.
 //
 // k_moe_up:   every cluster works out the routing for itself (its CTAs share the experts' logits through distributed shared memory), then the CTAs

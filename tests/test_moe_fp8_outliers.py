@@ -50,3 +50,34 @@ def test_inner_values_beyond_fp32_are_infinite(hidden, inner, x_type):
     rest = [0, 2, 3]
     check(x[rest], lay, 1, call(x[rest], lay, 1))
     assert all(torch.equal(y[t], v) for t, v in zip(rest, call(x[rest], lay, 1)[0]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("x_type", [BF16, F32])
+def test_small_activations_beside_a_large_one_that_weighs_nothing(x_type):
+    """Activations are left with 2^-39 of the token's largest off (and 2^-23 of themselves): the largest is 2^20 and its weights are zero."""
+    hidden, inner, top_k = 640, 128, 2
+    router, gu, gus, down, ds = layer(4, hidden, inner, x_type, 61)
+    router[:, 100] = 0
+    gu[..., 100] = 0
+    x = tokens_of(3, hidden, x_type, 62)
+    x[:, 100] = 2.0 ** 20
+    y, ids, probs = call(x, (router, gu, gus, down, ds), top_k)
+    xd = x.double()
+    off = torch.maximum(2.0 ** -23 * xd.abs(), torch.full_like(xd, 2.0 ** -39 * 2.0 ** 20)) if x_type == F32 else torch.zeros_like(xd)
+    s_h, s_i = (158 + hidden / 64) * 2.0 ** -24, (158 + inner / 64) * 2.0 ** -24      # sums of a layer: see test_moe_fp8
+    for t in range(3):
+        ref, tol = torch.zeros(hidden, dtype=torch.float64, device="cuda"), torch.zeros(hidden, dtype=torch.float64, device="cuda")
+        for k in range(top_k):
+            e, p = int(ids[t, k]), float(probs[t, k])
+            wg, wu, wd = F.weight_values(gu[e, 0], gus[e, 0]), F.weight_values(gu[e, 1], gus[e, 1]), F.weight_values(down[e], ds[e])
+            a, b = wg @ xd[t], wu @ xd[t]
+            da, db = wg.abs() @ (s_h * xd[t].abs() + off[t]), wu.abs() @ (s_h * xd[t].abs() + off[t])
+            silu = a * torch.sigmoid(a)
+            v = silu * b
+            dv = 1.1 * da * (b.abs() + db) + silu.abs() * db + 10 * 2.0 ** -24 * v.abs()
+            ref += p * (wd @ v)
+            tol += p * (wd.abs() @ (dv + (s_i + 40 * 2.0 ** -24) * v.abs()))
+        if x_type == BF16:
+            tol += F.HALF_STEP[BF16] * (ref.abs() + tol)
+        assert bool(((y[t].double() - ref).abs() <= tol).all())
