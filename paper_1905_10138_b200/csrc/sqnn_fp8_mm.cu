@@ -22,6 +22,7 @@
 // stream; large ones by the two accumulators that take turns: per two blocks 600 cycles of MMA, and reading, scaling and signalling 1200 that overlap only in part.
 #include "sqnn_launch.h"
 #include "sqnn_fp8.cuh"
+#include "sqnn_fp8_plan.h"
 #include "sqnn_cluster.cuh"
 #include "sqnn_tc.cuh"
 
@@ -700,23 +701,6 @@ struct AtOnce {
         return (uint32_t)v;
     }
 };
-// The runtime counts one CTA with tensor memory per SM.  More are there at once where shared and tensor memory allow: 228 KB, of which a CTA
-// takes 1 KB and its static variables besides, and 512 columns.
-constexpr uint32_t ctas_per_sm(size_t smem, uint32_t tmem_cols)
-{
-    const uint32_t by_smem = (uint32_t)(228 * 1024 / (smem + 1536)), by_tmem = 512 / tmem_cols;
-    return by_smem < by_tmem ? by_smem : by_tmem;
-}
-// CTAs (or pairs) per tile: enough for `wanted` of them in all, as far as all clusters run at once (a second wave costs more than the split
-// gains: 4096 x 9216 batch 64 by clusters of four, 128 CTAs, 12.4 us; of six and eight, in two waves, 19 and 25).
-template <typename F>
-uint32_t split_for(uint32_t tiles, uint32_t wanted, uint32_t most, const F &at_once)
-{
-    uint32_t split = 1;
-    while (tiles * split < wanted && split < most && tiles <= at_once(split + 1)) ++split;
-    return split;
-}
-
 template <bool SWAP, uint32_t N>
 size_t smem_of(uint32_t split, uint32_t stages)
 {
@@ -738,7 +722,7 @@ int launch_fp8(Fp8Args M, const Operands &O, uint32_t wanted, int dev, cudaStrea
     M.split = split_for(M.tiles, wanted, M.kblocks < 8 ? M.kblocks : 8,
                         [&](uint32_t s) {
                             const size_t smem = smem_of<SWAP, N>(s, stages);
-                            return at_once(dev, kernel, s, threads_of_fp8<N>, smem) * ctas_per_sm(smem, tmem_cols_of<N>);
+                            return clusters_at_once(at_once(dev, kernel, s, threads_of_fp8<N>, smem), s, (uint32_t)sm_count(), ctas_per_sm(smem, tmem_cols_of<N>));
                         });
     CUtensorMap wmap, xmap;
     if (!make_map(&wmap, O.w, O.n, M.m, O.ldw, SWAP ? LANES : N) || !make_map(&xmap, O.x, O.n, M.batch, O.ldx, SWAP ? N : LANES)) return SQNN_E_CUDA;
