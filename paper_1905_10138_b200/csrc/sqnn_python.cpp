@@ -13,6 +13,8 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <numeric>
+
 #include "sqnn.h"
 
 namespace {
@@ -413,8 +415,12 @@ PyObject *moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         const int64_t most = 1ll << 31;
         if (tokens >= most || experts >= most || top_k < 0 || top_k >= most || hidden >= most || inner >= most) { fail("too large"); return nullptr; }
         if (!stream_arg(a[13], &st)) return nullptr;
-        // the stride of a dimension of one element is whatever torch says: 0 suits every check
+        // the stride of a dimension of one element is whatever torch says: 0 suits every check, and as a row's what the other strides are multiples of
         const auto stride = [](const at::Tensor *t, int64_t d, int64_t one) { return t->size(d) == 1 ? one : t->stride(d); };
+        const auto row_of = [](int64_t half, int64_t expert, int64_t cols) {
+            const int64_t common = std::gcd(half, expert);
+            return common ? common : (cols + 15) / 16 * 16;
+        };
         sqnn_moe L = {};
         L.experts = (uint32_t)experts; L.top_k = (uint32_t)top_k; L.hidden = (uint32_t)hidden; L.inner = (uint32_t)inner;
         L.renormalize = (uint32_t)renormalize;
@@ -422,8 +428,8 @@ PyObject *moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         L.gate_up = ptr<uint8_t>(gu); L.gate_up_scale = ptr<float>(gus);
         L.down = ptr<uint8_t>(down); L.down_scale = ptr<float>(downs);
         L.router_row = row_stride(router);
-        L.gate_up_expert = stride(gu, 0, 0); L.gate_up_half = gu->stride(1); L.gate_up_row = stride(gu, 2, (hidden + 15) / 16 * 16);
-        L.down_expert = stride(down, 0, 0); L.down_row = stride(down, 1, (inner + 15) / 16 * 16);
+        L.gate_up_expert = stride(gu, 0, 0); L.gate_up_half = gu->stride(1); L.gate_up_row = stride(gu, 2, row_of(L.gate_up_half, L.gate_up_expert, hidden));
+        L.down_expert = stride(down, 0, 0); L.down_row = stride(down, 1, row_of(0, L.down_expert, inner));
         const void *const p_x = ptr<void>(x);
         void *const p_y = ptr<void>(y), *const p_ws = ptr<void>(ws);
         int32_t *const p_ids = ptr<int32_t>(ids);
