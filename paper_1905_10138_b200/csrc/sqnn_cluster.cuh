@@ -18,12 +18,6 @@ SQNN_DEV uint32_t peer_addr(uint32_t sa, uint32_t rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(sa), "r"(rank));
     return a;
 }
-SQNN_DEV float4 peer_load4(uint32_t a)
-{
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
-    return v;
-}
 SQNN_DEV uint32_t peer_load(uint32_t a)
 {
     uint32_t v;

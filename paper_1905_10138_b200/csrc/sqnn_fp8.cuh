@@ -2,6 +2,8 @@
 #pragma once
 #include "sqnn_decode.cuh"
 
+#include <cuda_bf16.h>
+
 namespace sqnn {
 
 constexpr uint32_t FP8_BLOCK = SQNN_FP8_BLOCK;   // columns (and, of weights, rows) that share a scale
@@ -13,6 +15,12 @@ SQNN_DEV uint32_t to_fp8x2(float lo, float hi)
     uint16_t v;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(v) : "f"(hi), "f"(lo));
     return v;
+}
+
+SQNN_DEV uint32_t bf16x2(float lo, float hi)
+{
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return reinterpret_cast<const uint32_t &>(b);
 }
 
 }  // namespace sqnn

@@ -121,11 +121,6 @@ struct Sums {
     }
 };
 
-SQNN_DEV uint32_t bf16x2(float lo, float hi)
-{
-    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-    return reinterpret_cast<const uint32_t &>(b);
-}
 // Four neighbouring elements of a row of Y, as many of them as `room` allows.
 SQNN_DEV void put4(const Fp8Args &M, int64_t at, uint32_t room, const float4 &v)
 {
@@ -634,19 +629,6 @@ leave:
     if (warp == PW + 1) tmem_dealloc_pair(tmem_base, 512);
 }
 
-// Raises nothing when it fails; `rows` x n bytes with `ld` bytes from row to row, boxes of `box_rows` x 128 bytes, swizzled.
-bool make_map(CUtensorMap *map, const void *p, uint64_t n, uint64_t rows, int64_t ld, uint32_t box_rows)
-{
-    EncodeTiledFn encode = encode_tiled_fn();
-    if (!encode) return false;
-    const cuuint64_t gdim[2] = {(cuuint64_t)n, (cuuint64_t)rows};
-    const cuuint64_t gstride[1] = {(cuuint64_t)ld};
-    const cuuint32_t box[2] = {KB, box_rows};
-    const cuuint32_t estride[2] = {1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(p), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 int launch_clusters(const void *kernel, const CUtensorMap &first, const CUtensorMap &second, const Fp8Args &M, uint32_t grid, uint32_t cluster, uint32_t threads,
                     size_t smem, cudaStream_t st)
 {
@@ -725,7 +707,7 @@ int launch_fp8(Fp8Args M, const Operands &O, uint32_t wanted, int dev, cudaStrea
                             return clusters_at_once(at_once(dev, kernel, s, threads_of_fp8<N>, smem), s, (uint32_t)sm_count(), ctas_per_sm(smem, tmem_cols_of<N>));
                         });
     CUtensorMap wmap, xmap;
-    if (!make_map(&wmap, O.w, O.n, M.m, O.ldw, SWAP ? LANES : N) || !make_map(&xmap, O.x, O.n, M.batch, O.ldx, SWAP ? N : LANES)) return SQNN_E_CUDA;
+    if (!byte_rows_map(&wmap, O.w, O.n, M.m, O.ldw, SWAP ? LANES : N) || !byte_rows_map(&xmap, O.x, O.n, M.batch, O.ldx, SWAP ? N : LANES)) return SQNN_E_CUDA;
     return launch_clusters(kernel, SWAP ? wmap : xmap, SWAP ? xmap : wmap, M, M.tiles * M.split, M.split, threads_of_fp8<N>,
                            smem_of<SWAP, N>(M.split, stages), st);
 }
@@ -743,7 +725,7 @@ int launch_pair(Fp8Args M, const Operands &O, int dev, cudaStream_t st)
     const uint32_t pairs = at_once(1);
     if (pairs == 0) return SQNN_E_CUDA;
     CUtensorMap wmap, xmap;
-    if (!make_map(&wmap, O.w, O.n, M.m, O.ldw, LANES) || !make_map(&xmap, O.x, O.n, M.batch, O.ldx, LANES)) return SQNN_E_CUDA;
+    if (!byte_rows_map(&wmap, O.w, O.n, M.m, O.ldw, LANES) || !byte_rows_map(&xmap, O.x, O.n, M.batch, O.ldx, LANES)) return SQNN_E_CUDA;
     // Tiles of a last round that would leave most pairs idle are done as quarters, a CTA or a cluster each, by a kernel of their own (us, without / with:
     // 4096 x 9216 batch 1300, 22 of 96 tiles, 81.5 / 72.3; 2560 x 4096 batch 2048, 6 of 80, 46.5 / 39.5; 34 of 256 tiles: 4096 x 16384 batch
     // 4096 308 / 299, 4096 x 9216 180 / 173, but 8192 x 1024 batch 2048 37 / 39, so short rows keep to two thirds of the SMs).

@@ -1181,17 +1181,6 @@ MoeShape moe_shape(uint32_t tokens, uint32_t top_k, uint64_t inner)
     return s;
 }
 
-// Rows of 8-bit weights, boxes of `box_rows` by 128 columns, swizzled.
-bool make_map(CUtensorMap *map, const void *p, uint32_t n, uint64_t rows, int64_t ld, uint32_t box_rows)
-{
-    EncodeTiledFn encode = encode_tiled_fn();
-    if (!encode) return false;
-    const cuuint64_t gdim[2] = {n, rows}, gstride[1] = {(cuuint64_t)ld};
-    const cuuint32_t box[2] = {STEP, box_rows}, estride[2] = {1, 1};
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(p), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // Whether the second kernel has room for a ring of two slots, whatever the call: the sums of all tokens, slots of full groups.
 constexpr bool room_for_down(uint32_t rows, uint32_t warps)
 {
@@ -1222,8 +1211,8 @@ int launch_moe(MoeArgs M, const sqnn_moe *L, cudaStream_t st)
     const auto down = rows == 16 ? k_moe_down<16, MAX_DOWN_WARPS, false> : warps == 8 ? k_moe_down<32, 8, false> : k_moe_down<32, MAX_DOWN_WARPS, false>;
     const auto down_split = k_moe_down<16, MAX_DOWN_WARPS, true>;
     CUtensorMap gu_map, d_map;
-    if (!make_map(&gu_map, L->gate_up, M.hidden, (uint64_t)(M.experts - 1) * M.gu_expert + M.gu_half + M.inner, L->gate_up_row, 16) ||
-        !make_map(&d_map, L->down, M.inner, (uint64_t)(M.experts - 1) * M.d_expert + M.hidden, L->down_row, rows))
+    if (!byte_rows_map(&gu_map, L->gate_up, M.hidden, (uint64_t)(M.experts - 1) * M.gu_expert + M.gu_half + M.inner, L->gate_up_row, 16) ||
+        !byte_rows_map(&d_map, L->down, M.inner, (uint64_t)(M.experts - 1) * M.d_expert + M.hidden, L->down_row, rows))
         return SQNN_E_CUDA;
     if (ensure_dynamic_smem(reinterpret_cast<const void *>(up), SMEM_BYTES) != SQNN_OK) return SQNN_E_CUDA;
     cudaLaunchAttribute attr[2];

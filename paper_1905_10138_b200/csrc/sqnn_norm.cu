@@ -38,70 +38,10 @@ template <typename T> SQNN_DEV float to_f32(T v);
 template <> SQNN_DEV float to_f32<float>(float v) { return v; }
 template <> SQNN_DEV float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
 
-SQNN_DEV void load8(const float *p, float (&v)[8])
-{
-    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-SQNN_DEV void load8(const __nv_bfloat16 *p, float (&v)[8])
-{
-    const uint4 a = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) {
-        v[2 * j] = __uint_as_float(u[j] << 16);
-        v[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
-    }
-}
-SQNN_DEV void store8(float *p, const float (&v)[8])
-{
-    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-}
-SQNN_DEV uint32_t pack_bf16(float lo, float hi)
-{
-    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-    return reinterpret_cast<const uint32_t &>(b);
-}
-SQNN_DEV void store8(__nv_bfloat16 *p, const float (&v)[8])
-{
-    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-}
-
 // Where a thread's eight elements of a slot lie.  Sixteen threads share a group of 128 columns: with VEC each has eight in a row (16-byte
 // accesses; rows on 16-byte boundaries), without it every sixteenth (neighbouring threads on neighbouring elements, any alignment).
 template <bool VEC> SQNN_DEV uint32_t first_of(uint32_t unit) { return VEC ? unit * 8 : (unit >> 4) * 128 + (unit & 15); }
 template <bool VEC> constexpr uint32_t step_of = VEC ? 1 : 16;
-
-// Elements past n read as zero.
-template <typename T, bool VEC>
-SQNN_DEV void fetch(const T *row, uint32_t i, uint32_t n, float (&v)[8])
-{
-    if (VEC && i + 8 <= n) {
-        load8(row + i, v);
-    } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-            const uint32_t at = i + j * step_of<VEC>;
-            v[j] = at < n ? to_f32<T>(row[at]) : 0.0f;
-        }
-    }
-}
-SQNN_DEV void put(float *p, float v) { *p = v; }
-SQNN_DEV void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
-template <typename T, bool VEC>
-SQNN_DEV void store(T *row, uint32_t i, uint32_t n, const float (&v)[8])
-{
-    if (VEC && i + 8 <= n) {
-        store8(row + i, v);
-    } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 8; ++j) {
-            const uint32_t at = i + j * step_of<VEC>;
-            if (at < n) put(row + at, v[j]);
-        }
-    }
-}
 
 // Eight elements as they were loaded, so that a load can be asked for long before its numbers are looked at.
 template <typename T> struct Raw;
@@ -128,11 +68,45 @@ template <> struct Raw<__nv_bfloat16> {
     }
     SQNN_DEV void take(const float (&v)[8])
     {
-        a = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        a = make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
     }
     SQNN_DEV void put(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = a; }
     SQNN_DEV void load(const __nv_bfloat16 *p) { a = *reinterpret_cast<const uint4 *>(p); }
 };
+// Elements past n read as zero.
+template <typename T, bool VEC>
+SQNN_DEV void fetch(const T *row, uint32_t i, uint32_t n, float (&v)[8])
+{
+    if (VEC && i + 8 <= n) {
+        Raw<T> raw;
+        raw.load(row + i);
+        raw.values(v);
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+            const uint32_t at = i + j * step_of<VEC>;
+            v[j] = at < n ? to_f32<T>(row[at]) : 0.0f;
+        }
+    }
+}
+SQNN_DEV void put(float *p, float v) { *p = v; }
+SQNN_DEV void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+template <typename T, bool VEC>
+SQNN_DEV void store(T *row, uint32_t i, uint32_t n, const float (&v)[8])
+{
+    if (VEC && i + 8 <= n) {
+        Raw<T> raw;
+        raw.take(v);
+        raw.put(row + i);
+    } else {
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+            const uint32_t at = i + j * step_of<VEC>;
+            if (at < n) put(row + at, v[j]);
+        }
+    }
+}
+
 template <typename T, bool VEC>
 SQNN_DEV void request(Raw<T> &raw, const T *row, uint32_t unit, uint32_t units, uint32_t n)
 {

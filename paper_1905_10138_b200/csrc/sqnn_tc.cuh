@@ -13,6 +13,17 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 EncodeTiledFn encode_tiled_fn();
 
+// A tensor map of `rows` rows of n bytes, `ld` bytes from row to row: boxes of `box_rows` x 128 bytes, swizzled.
+inline bool byte_rows_map(CUtensorMap *map, const void *p, uint64_t n, uint64_t rows, int64_t ld, uint32_t box_rows)
+{
+    EncodeTiledFn encode = encode_tiled_fn();
+    if (!encode) return false;
+    const cuuint64_t gdim[2] = {(cuuint64_t)n, (cuuint64_t)rows}, gstride[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {128, box_rows}, estride[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(p), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 SQNN_DEV void mbar_init(uint32_t bar, uint32_t count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" :: "r"(bar), "r"(count) : "memory");
