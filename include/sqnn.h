@@ -425,7 +425,8 @@ typedef struct sqnn_moe {
  * to d_y ([tokens][hidden], row stride ldy, fully overwritten).  x_dtype (of d_x and router) and y_dtype:
  * SQNN_X_F32 or SQNN_X_BF16.  The experts and their order are those of the logits in 64 bits (exact products): logits are summed in fp32 over 64 (bf16) or 8 (fp32)
  * products and then in 64 bits, which leaves them off by at most 2^-20 of the sum of their products' magnitudes, and those of a token that lie nearer to one another
- * are computed once more in 64 bits; many such ones, or products beyond fp32's range, take longer.  The shares come from these logits.  fp32 activations are
+ * are computed once more in 64 bits; many such ones, or products beyond fp32's range, take longer.  (A router all of whose products with a token vanish in fp32 counts
+ * as zero, unless the token itself lies below 2^-60.)  The shares come from these logits.  fp32 activations are
  * taken to within 2^-23 of themselves or 2^-39 of the token's largest, whichever is more, bf16 ones exactly from 2^-31 of it on (else 2^-39 of it off), inner values to
  * within 2^-23 of themselves or 2^-39 of the largest of sixteen; all else is in fp32, and y is rounded to its type at the end.  Results are bit-identical from run to run.  A NaN among a token's logits counts
  * as the largest, so the layer always has top_k different experts.  d_ids and d_probs ([tokens][top_k], may be NULL) get the

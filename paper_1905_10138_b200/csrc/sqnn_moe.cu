@@ -198,6 +198,7 @@ SQNN_DEV void weights_of(uint32_t (&a)[4], uint32_t top, uint32_t bottom)
 // `scratch`: 24 KB.
 template <typename XT> constexpr float SLACK = sizeof(XT) == 2 ? 0x1.81p-21f : 0x1.01p-21f;
 constexpr uint32_t INFINITE = 0x7f800000u, UNKNOWN = 0x7f000000u;         // (2^127: a logit that has passed the range has an A above that)
+constexpr uint32_t ORDINARY = 67u << 23;                         // 2^-60
 // 64-bit floating numbers as integers of the same order; NaN comes last.  And back.
 SQNN_DEV int64_t key_of(double v)
 {
@@ -594,9 +595,10 @@ SQNN_DEV void choose(const MoeArgs &M, int64_t *keys, int64_t *chosen, Routing &
                 }
             }
             __syncwarp();
-            // Equal or nearly equal ones among these?  (Logits of zeros are zero; of infinities and NaN nothing better is to be had.)
+            // Equal or nearly equal ones among these?  (Logits of zeros are zero, those of a router that leaves nothing of a token count as zero; of infinities and
+            // NaN nothing better is to be had.)
             const uint32_t largest = R.largest[t], spread = R.spread[t];
-            if (settled || largest == 0 || largest >= INFINITE) break;
+            if (settled || largest == 0 || largest >= INFINITE || (spread == 0 && largest >= ORDINARY)) break;
             const float slack = __uint_as_float(spread < UNKNOWN ? spread : INFINITE) * (2 * SLACK<XT>) + 0x1p-124f * (float)M.hidden;
             int64_t left = LOWEST;                                    // the largest that is left, lane by lane
             for (uint32_t e = lane; e < M.experts; e += 32) left = max(left, keys[t * M.experts + e]);
