@@ -17,9 +17,10 @@
 // columns, through distributed shared memory, and these add them up in the order of the ranks.  No workspace, no atomics: results are the same
 // from run to run.
 //
-// Measured (floor at the copy's and the tensor cores' measured rates): 4096 x 9216 batch 1 9.9 us (5.8), batch 64 12.5 us (6.0), 4096 x 16384 batch 512
-// 49 us (20.6), batch 4096 299 to 312 us (164).  Small batches are bound by how soon the loads start and by the end of the call (start, exchange of sums) beside the
-// stream; large ones by the two accumulators that take turns: per two blocks 600 cycles of MMA, and reading, scaling and signalling 1200 that overlap only in part.
+// Measured, us (floor at the copy's and the tensor cores' measured rates): 4096 x 9216 batch 1 9.9 (5.8), batch 64 12.7 (6.0); 4096 x 16384 batch 512 42.5 (20.6) in
+// short runs and 49 in loops of a second, where the chip is at its 1000 W and the clock at 1.69 GHz; batch 4096 275 (164) and 314 (at 1.49 GHz).  Small batches are bound by
+// how soon the loads start and by the end of the call (start, exchange of sums) beside the stream; large ones by the two accumulators that take turns (per two
+// blocks 600 cycles of MMA, and reading, scaling and signalling 1200 that overlap only in part) and, in long loops, by power.
 #include "sqnn_launch.h"
 #include "sqnn_fp8.cuh"
 #include "sqnn_fp8_plan.h"
@@ -290,8 +291,8 @@ SQNN_DEV void add_sums(const Fp8Args &M, const float *buffer, uint32_t share, ui
 SQNN_DEV void tmem_request(uint32_t taddr, uint32_t (&v)[16]) { tmem_request16(taddr, v); }
 SQNN_DEV void tmem_request(uint32_t taddr, uint32_t (&v)[32]) { tmem_request32(taddr, v); }
 // acc += t * scale of this block.  A thread's COLS columns come in pieces, each asked for before the arithmetic of the one before; `release` is called
-// when the last one has arrived.  (What bounds this is power: at 4096 x 16384 and batch 4096 the chip is at its limit of 1000 W.  Single fma take
-// fewer cycles than fma.rn.f32x2, 385 against 525 a block of 128 columns with nothing else running, but did not fit the registers here.)
+// when the last one has arrived.  (Single fma take fewer cycles than fma.rn.f32x2, 385 against 525 a block of 128
+// columns with nothing else running, but did not fit the registers here.)
 template <bool SWAP, uint32_t COLS, typename F>
 SQNN_DEV void promote(Sums<COLS> &acc, uint32_t tmem_at, const float *s, float lane_s, const F &release)
 {
@@ -726,9 +727,9 @@ int launch_pair(Fp8Args M, const Operands &O, int dev, cudaStream_t st)
     if (pairs == 0) return SQNN_E_CUDA;
     CUtensorMap wmap, xmap;
     if (!byte_rows_map(&wmap, O.w, O.n, M.m, O.ldw, LANES) || !byte_rows_map(&xmap, O.x, O.n, M.batch, O.ldx, LANES)) return SQNN_E_CUDA;
-    // Tiles of a last round that would leave most pairs idle are done as quarters, a CTA or a cluster each, by a kernel of their own (us, without / with:
-    // 4096 x 9216 batch 1300, 22 of 96 tiles, 81.5 / 72.3; 2560 x 4096 batch 2048, 6 of 80, 46.5 / 39.5; 34 of 256 tiles: 4096 x 16384 batch
-    // 4096 308 / 299, 4096 x 9216 180 / 173, but 8192 x 1024 batch 2048 37 / 39, so short rows keep to two thirds of the SMs).
+    // Tiles of a last round that would leave most pairs idle are done as quarters, a CTA or a cluster each, by a kernel of their own (us, without / with, in turn on
+    // one chip: 4096 x 9216 batch 1300, 22 of 96 tiles, 78.1 / 68.2; 2560 x 4096 batch 2048, 6 of 80, 41.5 / 33.7; 34 of 256 tiles: 4096 x 9216 batch 4096 157.8 / 154.5,
+    // 4096 x 16384 284 to 305 / 275 to 283; but 8192 x 1024 batch 2048 37 / 39, so short rows keep to two thirds of the SMs).
     const uint32_t last = M.split == 1 && M.tiles > pairs ? M.tiles % pairs : 0;
     const bool tail = last > 0 && 4 * last <= (M.kblocks < 64 ? (uint32_t)sm_count() * 2 / 3 : (uint32_t)sm_count());
     if (tail) M.tiles -= last;
@@ -770,8 +771,8 @@ int fp8_matmul_queue(uint64_t m, uint64_t n, uint32_t batch, const uint8_t *d_w,
     if (w_tiles * x_tiles > 0x7fffffffull / 8) return SQNN_E_UNSUPPORTED;
     const uint32_t sms = (uint32_t)sm_count();
     // Small batches: a quarter more CTAs than SMs keep enough weights on their way; those with more columns are one to an SM.  The pair's larger
-    // tiles gain from about as many 128 x 128 tiles on as there are SMs (us, pair / one CTA per tile: 4096 x 16384 batch 512 40.7 / 45.3, 8192 x
-    // 1024 batch 2048 35.0 / 40.8; 6000 x 3000 batch 200 15.2 / 11.5, 2048 x 2048 batch 256 11.6 / 7.8).
+    // tiles gain from about as many 128 x 128 tiles on as there are SMs (us, pair / one CTA per tile, in turn on one chip: 4096 x 16384 batch 512 42.5 / 48.0, 8192 x
+    // 1024 batch 2048 35.4 / 40.3, 4096 x 9216 batch 4096 155 / 187; 6000 x 3000 batch 200 17.0 / 11.6, 2048 x 2048 batch 256 14.6 / 9.8).
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SQNN_E_CUDA;
     if (batch <= 16) return launch_fp8<true, 16>(M, O, sms * 5 / 4, dev, st);

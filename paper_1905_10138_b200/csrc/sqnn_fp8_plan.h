@@ -21,7 +21,7 @@ constexpr uint32_t clusters_at_once(uint32_t runtime_says, uint32_t cluster, uin
 }
 
 // CTAs (or pairs) per tile: enough for `wanted` of them in all, as far as all clusters run at once (a second wave costs more than the split
-// gains: 4096 x 9216 batch 64 by clusters of four, 128 CTAs, 12.4 us; of six and eight, in two waves, 19 and 25).
+// gains: 4096 x 9216 batch 64 by clusters of four, 128 CTAs, 12.7 us; of six and eight, in two waves, 19 and 25).
 template <typename F>
 uint32_t split_for(uint32_t tiles, uint32_t wanted, uint32_t most, const F &at_once)
 {

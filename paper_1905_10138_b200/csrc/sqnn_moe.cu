@@ -9,7 +9,7 @@
 // of mma.sync m16n8k16 with up to eight tokens as the columns of B.  (mma.sync, not tcgen05: weights that are used once gain nothing
 // from a tile that many warps share, and the rate of mma.sync is several times what memory asks for.  Weights read straight into registers, 62 us
 // for one token and 8 of 64 experts of 2048 x 1024: the unrolled code did not fit the instruction cache.  A ring filled by 16-byte copies of
-// every lane, 38 us: 230 to 280 instructions per kilobyte or two, most of them addresses.  This form: 26 us.)
+// every lane, 38 us: 230 to 280 instructions per kilobyte or two, most of them addresses.  This form: 26.3 us.)
 // The 16 columns of an MMA are dealt so that its k slots 2 t, 2 t + 1, 2 t + 8, 2 t + 9 are columns 4 t .. 4 t + 3, and B is stored
 // in the order that gives a lane its share of four MMAs in 32 bytes: position 16 t + 4 j + i of 64 holds column 16 j + 4 t + i.
 //
@@ -19,8 +19,8 @@
 // MMA: a unit of the first kernel is the 16 inner values of one MMA of the second.
 // Sums are fp32 in the MMA, then scaled and added to 32-bit sums.
 //
-// k_moe_up:   every cluster works out the routing for itself (its CTAs share the experts' logits through distributed shared memory), then the CTAs
-//             share all units (expert, 16 rows of G and the same of U); a CTA's warps share the columns of up to 16 units at a time.
+// k_moe_up:   every cluster works out the routing for itself (its CTAs share the experts' logits through distributed shared memory; 18 tokens of 128 experts: a third of
+//             the call), then the CTAs share all units (expert, 16 rows of G and the same of U); a CTA's warps share the columns of up to 16 units at a time.
 // k_moe_down: a CTA, or a cluster of two or four, has 16 or 32 rows of all chosen experts' D; the warps share (expert, 128 columns) evenly; each sums into its own
 //             accumulators, which are added up in warp and rank order.
 // No atomics on sums: results are the same from run to run.
@@ -1203,7 +1203,7 @@ int launch_moe(MoeArgs M, const sqnn_moe *L, cudaStream_t st)
     // second kernel: 32 rows per CTA where that still makes two CTAs for three SMs; as deep a ring as there is room for
     const uint32_t rows = 3 * ((M.hidden + 31) / 32) >= 2 * (uint32_t)sm_count() ? 32 : 16;
     M.slot = rows * STEP + (M.tokens < M.per ? M.tokens : M.per) * H_PITCH;
-    // 12 warps with a ring of two slots (16 tokens, 64 experts of 1536, top 8, hidden 4096: 209 us) are faster than 8 with four (213), but do not
+    // 12 warps with a ring of two slots (16 tokens, 64 experts of 1536, top 8, hidden 4096: 209 us in short runs) are faster than 8 with four (213), but do not
     // always fit; 8 with two do, and so do 12 where a CTA has 16 rows
     const auto depth_of = [&](uint32_t warps) { return (uint32_t)((DOWN_SMEM_BYTES - 1024 - (size_t)warps * M.tokens * rows * 4) / (warps * M.slot)); };
     static_assert(room_for_down(16, MAX_DOWN_WARPS) && room_for_down(32, 8), "a ring of two slots whatever the call");

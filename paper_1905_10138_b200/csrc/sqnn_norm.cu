@@ -12,8 +12,9 @@
 //   - y / s is p c with c = rstd / (2^k s) in fp32: five roundings, less than 6 2^-24 off.  It is converted from both ends of what that allows (c (1 -+
 //     2^-21)); only where these give two numbers (12 of a million values) is it computed once more in 64 bits.
 // Every operand is read once and every result written once; a row stays in registers between its two passes.  8192 rows of 4096, bf16 with
-// residual: 58 us (36 us at the copy's rate); instructions bound it, about 25 for an element.  A first form took 108 us: a block per row with nothing of
-// the next one on its way, tests of the distance to the border by bits, 64-bit indexes.
+// residual: 58 us (36 us at the copy's rate).  About 25 instructions an element fill 64 % of the issue slots; the rest is latency: a row has two barriers and one
+// warp's work between its passes (2.8 of 11.4 warps wait at a barrier for each that issues), and 64 registers leave 32 warps an SM to hide it.  A first form took 108 us:
+// a block per row with nothing of the next one on its way, tests of the distance to the border by bits, 64-bit indexes.
 #include "sqnn_launch.h"
 #include "sqnn_fp8.cuh"
 
@@ -358,7 +359,8 @@ __global__ void __launch_bounds__(MOST, MOST == 384 ? 3 : SLOTS == 1 || (SLOTS =
 // One slot of eight elements a thread, as far as 512 threads go, else as many as a row needs.  Many rows of which a thread loads no more than four bytes an
 // element, on 16-byte boundaries: two slots, so that the reductions weigh less (8192 x 4096, bf16 with residual: one slot 59 us, two 56, four 71; at 2000 rows
 // 17.3 and 18.7; 8000 x 2944 52 and 46, 2000 x 2944 16.3 and 15.4).  fp32 or unaligned rows have no registers to spare for two (8000 x 3001, fp32 and bf16 residual, bf16 y: 96 us
-// with one, 166 with two; 8000 x 4096 66 and 76).  Where unaligned rows need two slots, two blocks to an SM (2000 x 5001, the same types: 58 us, one block 88).
+// with one, 166 with two; 8000 x 4096 66 and 76).  Where unaligned rows need two slots, two blocks to an SM (2000 x 5001, the same types: 58 us, one block 88).  The bound of 64
+// registers that this takes makes the two-slot forms spill (fp32 and unaligned ones up to 212 bytes a thread); other sizes and types of them were not measured apart.
 template <typename XT, typename RT, typename WT, bool RES>
 int launch_norm(const NormArgs &A, uint32_t batch, bool vec, cudaStream_t st)
 {
