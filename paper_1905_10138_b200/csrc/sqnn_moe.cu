@@ -17,7 +17,7 @@
 // are exact down to 2^-31 of the largest, fp32 numbers, in two, are left with 2^-23 of themselves off, or 2^-39 of the largest (as bf16 numbers are below).  (A
 // third MMA would bring the last bit; the weights have four.)  x is scaled per token, the inner values, whose largest nobody knows before all are there, per token and
 // MMA: a unit of the first kernel is the 16 inner values of one MMA of the second.
-// Sums are fp32 in the MMA, then scaled and added to 32-bit sums.
+// Sums are fp32 in the MMA (cut to it, not rounded), then scaled and added to 32-bit sums.
 //
 // k_moe_up:   every cluster works out the routing for itself (its CTAs share the experts' logits through distributed shared memory; 18 tokens of 128 experts: a third of
 //             the call), then the CTAs share all units (expert, 16 rows of G and the same of U); a CTA's warps share the columns of up to 16 units at a time.
